@@ -1,14 +1,17 @@
 /*
  * ta.h — C ABI of the Transactional Attention (TA) KV-cache compaction library for NVIDIA B200 (sm_100a).
  *
- * The library implements one thing: the retention step of TA (Algorithm 1), run once over a prefilled KV cache,
- * per layer and per KV head:
+ * The library implements the retention step of TA (Algorithm 1), run once over a prefilled KV cache, per layer and per
+ * KV head:
  *
  *   1. anchor detection + voucher allocation   (Section 3.2, Eq. 2, Algorithm 1 steps 1-6)   ta_sponsor_mask
  *   2. attention part of the utility           (Eq. 1 terms alpha*A_i and delta*P_i)           ta_score
  *   3. budget-K selection                      (Algorithm 1 step 8, Section 3.3)               ta_select_topk
  *   4. eviction = gather of retained rows      (Algorithm 1 step 9, Section 3.2)               ta_compact_kv
  *   all four in one enqueue                    (Algorithm 1)                                   ta_compress
+ *
+ * and, for the decode loop that goes on with the retained rows, rotary positions (ta_rotate), a cache of 16 or 8 bits in
+ * pages (ta_cache_append, ta_cache_read) and the attention of new tokens over it (ta_attend).
  *
  * Conventions shared by every entry point
  *   - Positions are 0-based; the paper's 1-based position i is i0 + 1.
@@ -462,6 +465,118 @@ ta_status ta_stream_step(ta_ctx* ctx, const ta_patterns* pats, const ta_policy* 
 ta_status ta_ctx_selftest_step_wait(ta_ctx* ctx, const ta_patterns* pats, const ta_policy* policy, ta_stream* st /*HOST*/,
                                     const int32_t* new_ids, const float* attn, int32_t* evicted_pos, uint64_t limit_ns,
                                     void* stream);
+
+/* ---- after the retention decision: rotary positions, the cache, attention of new tokens ----------------------------
+ * (No counterpart in the paper, whose Section 3.1 takes a cache and its attention as given.) What a decode step does next
+ * to the retained rows: rotate the new token's queries and keys, write its key and value into the cache, in as many bits
+ * as the cache has, and attend over the rows that are there. The attention mass per cache row that ta_attend returns is
+ * what ta_stream_step takes. */
+
+/* Rotary positions. Coordinates a and b of a pair turn by an angle that is the pair's frequency times the position:
+ *   (a, b) -> magnitude * (a cos - b sin, a sin + b cos);   inverse: the angle is negated.
+ * With the same magnitude the inverse is the transpose: it takes a gradient of the rotated values to one of the values,
+ * and with 1 / magnitude it undoes the rotation. The first d_rot coordinates of a head are rotated, the others kept.
+ * Frequencies are turns per position as 64-bit fractions, phase[i] = round down(turns * 2^64), so that an angle is the
+ * product position * phase modulo 2^64: exact in every int32 position, negative ones among them (positions far into a
+ * context lose nothing, as they do where position * frequency is rounded to 32 bits). Sine and cosine are taken of the
+ * product's upper 32 bits; values are rotated in 32 bits and rounded once. */
+enum { TA_ROTARY_HALF = 0,       /* pairs (i, i + d_rot/2) */
+       TA_ROTARY_INTERLEAVED = 1 /* pairs (2i, 2i + 1)     */ };
+typedef struct ta_rotary {
+  const uint64_t* phase;    /* DEVICE [d_rot / 2], as written by ta_rotary_table                                          */
+  const int32_t* positions; /* DEVICE, one per token of the call (packed like token_ids), or NULL: see each call          */
+  int32_t d_rot;            /* a multiple of 8, 8 <= d_rot <= d                                                           */
+  int32_t layout;           /* TA_ROTARY_HALF or TA_ROTARY_INTERLEAVED                                                    */
+  int32_t inverse;
+  float magnitude;          /* finite                                                                                     */
+} ta_rotary;
+
+/* Frequencies base^(-2i / d_rot) radians per position, scaled for contexts that are longer than the trained ones:
+ *   TA_SCALING_PLAIN   as they are (factor, original_len, low and high are not read)
+ *   TA_SCALING_LINEAR  divided by factor (position interpolation)
+ *   TA_SCALING_BASE    base * factor^(d_rot / (d_rot - 2)) in place of base
+ *   TA_SCALING_RAMP    between both by the pair's index: pairs up to the one that turns `high` times within original_len
+ *                      positions keep their frequency, those from the one that turns `low` times on are divided by factor,
+ *                      linear in between (the two indices rounded outwards); *magnitude = 0.1 ln(factor) + 1 (YaRN)
+ *   TA_SCALING_BAND    the same with the weight taken from the pair's own turns within original_len: (turns - low) /
+ *                      (high - low), clipped to [0, 1], is the share of the unscaled frequency
+ * phase is HOST [d_rot / 2], magnitude HOST. base > 1; factor >= 1, original_len > 0, 0 < low < high where they are read. */
+enum { TA_SCALING_PLAIN = 0, TA_SCALING_LINEAR = 1, TA_SCALING_BASE = 2, TA_SCALING_RAMP = 3, TA_SCALING_BAND = 4 };
+ta_status ta_rotary_table(int d_rot, double base, int scaling, double factor, double original_len, double low, double high,
+                          uint64_t* phase /*HOST*/, float* magnitude /*HOST*/);
+
+/* Rotates the queries and the keys of a batch in one enqueue.
+ *   q, q_out  views with Hq heads; k, k_out views with Hkv heads, or Hkv = 0 and no k (ptr NULL)
+ * An output view may be the input view itself (same pointer and strides); other overlaps are not allowed. positions NULL:
+ * token i of a sequence has position i. d a multiple of 8, at most TA_MAX_ROTATE_DIM; views are ragged where the batch is. */
+enum { TA_MAX_ROTATE_DIM = 256 };
+ta_status ta_rotate(ta_ctx* ctx, const ta_batch* batch, int Hq, int Hkv, int d, const ta_rotary* rotary /*HOST*/,
+                    ta_bf16_view q, ta_bf16_view q_out, ta_bf16_view k, ta_bf16_view k_out, void* stream);
+
+/* A cache of key and value rows, in pages or dense, in one of three formats:
+ *   TA_CACHE_BF16  rows of d bf16
+ *   TA_CACHE_E4M3  rows of d 8-bit floats (4 exponent, 3 mantissa bits) and an fp32 scale per row
+ *   TA_CACHE_INT8  rows of d whole numbers -127..127 and an fp32 scale per row
+ * Row r of sequence b, layer l and KV head g lies in page table[b * pages_per_seq + r / page], at
+ *   k + l*stride_l + page_id*stride_p + g*stride_h + (r % page)*stride_r   (elements; v likewise, scales with their own)
+ * table NULL: the sequence's pages are b * pages_per_seq + r / page (with page rows a sequence: one dense row block each).
+ * Strides in elements, multiples of 16 bytes (scale strides: any), not negative; k and v 16-byte aligned; d 64 or 128. What
+ * a table holds behind the pages that a call reaches is not read. */
+enum { TA_CACHE_BF16 = 0, TA_CACHE_E4M3 = 1, TA_CACHE_INT8 = 2 };
+typedef struct ta_cache {
+  void *k, *v;               /* DEVICE */
+  float *k_scale, *v_scale;  /* DEVICE, NULL for TA_CACHE_BF16 */
+  int64_t stride_l, stride_p, stride_h, stride_r;
+  int64_t scale_stride_l, scale_stride_p, scale_stride_h, scale_stride_r;
+  const int32_t* table;      /* DEVICE [batch][pages_per_seq], or NULL */
+  const int32_t* lens;       /* DEVICE [batch], or [n_layers][batch][Hkv] where lens_per_unit, or NULL: len_uniform each */
+  int32_t n_layers, batch, Hkv, d;
+  int32_t format, page, n_pages, pages_per_seq;
+  int32_t lens_per_unit;
+  int32_t len_uniform;       /* HOST scalar */
+} ta_cache;
+
+/* Writes the keys and values of batch->n_layers (= cache->n_layers) layers' new tokens into the cache.
+ *   k, v    bf16 views, positions = new tokens, heads = Hkv; ragged where the batch is
+ *   rotary  rotates the keys on their way (HOST; positions NULL: a token's position is its row), or NULL
+ *   rows    DEVICE int32 [L][B][Hkv][n_uniform], or [L][Hkv][total_tokens] where the batch is ragged: the row of every token,
+ *           negative: not written; NULL: token i of a sequence goes to row lens + i. The lengths are not changed.
+ * A row of an 8-bit cache: with m the largest magnitude, at least 2^-100, and F = 448 (E4M3) or 127 (INT8), scale = m / F
+ * and code = x * (F / m) rounded to nearest even, in 32 bits. A row with a NaN or an infinity gets scale NaN and so reads
+ * back as NaN. Keys that are rotated are rounded once, to the cache's format. No two tokens of a call may share a row.
+ * A row beyond the table, or in a page outside 0..n_pages-1, is not written and reported (TA_ERR_DEVICE_BOUNDS). */
+ta_status ta_cache_append(ta_ctx* ctx, const ta_cache* cache, const ta_batch* batch, const ta_rotary* rotary, ta_bf16_view k,
+                          ta_bf16_view v, const int32_t* rows, void* stream);
+
+/* Reads rows back as bf16 (code * scale rounded once): also a retention step's gather out of a paged cache.
+ *   rows          as for ta_cache_append, negative: a row of zeros; NULL: token i of a sequence is row i
+ *   k_out, v_out  bf16 views, out; ragged where the batch is; heads = Hkv
+ * Rows outside the table or the pages give zeros and are reported. Lengths are not read. */
+ta_status ta_cache_read(ta_ctx* ctx, const ta_cache* cache, const ta_batch* batch, const int32_t* rows, ta_bf16_view k_out,
+                        ta_bf16_view v_out, void* stream);
+
+/* Attention of T new tokens per sequence over the cache.
+ *   n = lens + new_rows rows of every sequence (or unit) are there; query t of T sees the first n - (T-1-t) of them where
+ *   causal, all n otherwise; query head h belongs to KV head h / (Hq / Hkv).
+ *     s_j = scale * <q, k_j>,   p = softmax over the visible rows,   out = sum_j p_j v_j
+ *   q, out  bf16 views [l][b][Hq][T]; out is written as bf16 rounded once from 32 bits
+ *   rotary  rotates the queries on their way (HOST; positions DEVICE [batch][T], NULL: n - T + t), or NULL
+ *   scale   0 means 1 / sqrt(d)
+ *   lse     DEVICE float [L][B][Hq][T], natural log, out; or NULL
+ *   mass    DEVICE float [L][B][Hkv][mass_stride], out, or NULL: sum of p_j over the unit's query heads and tokens, zero for
+ *           rows n..mass_stride-1 (mass_stride >= max_len): ta_stream_step's `attn` with mass_stride = K+1
+ *   max_len >= every n
+ * A query that sees no row gets out 0, lse -infinity and adds no mass. What rows beyond a query's last one hold, NaN
+ * included, has no influence on it. A sequence with n > max_len or beyond its table is cut there, and rows in a page
+ * outside 0..n_pages-1 are left out; both are reported (TA_ERR_DEVICE_BOUNDS). T <= TA_MAX_NEW_TOKENS, Hq / Hkv <= 256,
+ * max_len <= TA_MAX_SEQ_LEN. Products are of bf16 values (8-bit codes are exact in them; probabilities and rotated queries
+ * keep 16 bits), sums and softmax statistics are in 32 bits. Scratch: ta_attend_scratch_bytes (not kept between calls; what
+ * ta_compress keeps under a seq_epoch is dropped). */
+enum { TA_MAX_NEW_TOKENS = 64 };
+ta_status ta_attend_scratch_bytes(const ta_cache* cache, int Hq, int T, int max_len, int with_mass, size_t* out_bytes);
+ta_status ta_attend(ta_ctx* ctx, const ta_cache* cache, int Hq, int T, int new_rows, int max_len, int causal, float scale,
+                    const ta_rotary* rotary, ta_bf16_view q, ta_bf16_view out, float* lse, float* mass, int64_t mass_stride,
+                    void* stream);
 
 /* ---- host-buffer variant of ta_compress --------------------------------------------------------------------
  * Same computation with every data pointer on the HOST (pinned memory makes the copies asynchronous):

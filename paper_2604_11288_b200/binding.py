@@ -24,6 +24,9 @@ TA_ERR_CUDA, TA_ERR_TIMEOUT, TA_ERR_DEVICE_BOUNDS = 5, 6, 7
 TA_MODE_SCORED, TA_MODE_FAST = 0, 1
 TA_FLAG_ANCHOR_TOKEN, TA_FLAG_ANCHOR_END, TA_FLAG_SPONSORED = 1, 2, 4
 TA_PRESET_THEOREM, TA_PRESET_SEC33, TA_PRESET_AUDIT = 0, 1, 2
+TA_ROTARY_HALF, TA_ROTARY_INTERLEAVED = 0, 1
+TA_SCALING_PLAIN, TA_SCALING_LINEAR, TA_SCALING_BASE, TA_SCALING_RAMP, TA_SCALING_BAND = 0, 1, 2, 3, 4
+TA_CACHE_BF16, TA_CACHE_E4M3, TA_CACHE_INT8 = 0, 1, 2
 
 
 class ta_policy(C.Structure):
@@ -50,6 +53,20 @@ class ta_stream(C.Structure):
                 ("A", C.c_void_p), ("P", C.c_void_p), ("V", C.c_void_p), ("S", C.c_void_p), ("next_slot", C.c_void_p),
                 ("n_seen", C.c_void_p), ("hist", C.c_void_p), ("tok_ring", C.c_void_p), ("anc_B", C.c_void_p),
                 ("anc_L", C.c_void_p)]
+
+
+class ta_rotary(C.Structure):
+    _fields_ = [("phase", C.c_void_p), ("positions", C.c_void_p), ("d_rot", C.c_int32), ("layout", C.c_int32),
+                ("inverse", C.c_int32), ("magnitude", C.c_float)]
+
+
+class ta_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("stride_l", C.c_int64), ("stride_p", C.c_int64), ("stride_h", C.c_int64), ("stride_r", C.c_int64),
+                ("scale_stride_l", C.c_int64), ("scale_stride_p", C.c_int64), ("scale_stride_h", C.c_int64),
+                ("scale_stride_r", C.c_int64), ("table", C.c_void_p), ("lens", C.c_void_p), ("n_layers", C.c_int32),
+                ("batch", C.c_int32), ("Hkv", C.c_int32), ("d", C.c_int32), ("format", C.c_int32), ("page", C.c_int32),
+                ("n_pages", C.c_int32), ("pages_per_seq", C.c_int32), ("lens_per_unit", C.c_int32), ("len_uniform", C.c_int32)]
 
 
 class TAError(RuntimeError):
@@ -107,6 +124,24 @@ class _CtypesCalls:
                                               C.c_float(threshold), C.c_float(budget), int(span), int(rank_by_confidence),
                                               _ptr(flags), _ptr(voucher), _ptr(u_static), stream)
 
+    def ta_rotate(self, ctx, batch, Hq, Hkv, d, rotary, q, q_out, k, k_out, stream):
+        return self._lib.ta_rotate(ctx, C.byref(batch), Hq, Hkv, d, _ref(rotary), q, q_out, k, k_out, stream)
+
+    def ta_cache_append(self, ctx, cache, batch, rotary, k, v, rows, stream):
+        return self._lib.ta_cache_append(ctx, C.byref(cache), C.byref(batch), _ref(rotary), k, v, _ptr(rows), stream)
+
+    def ta_cache_read(self, ctx, cache, batch, rows, k_out, v_out, stream):
+        return self._lib.ta_cache_read(ctx, C.byref(cache), C.byref(batch), _ptr(rows), k_out, v_out, stream)
+
+    def ta_attend(self, ctx, cache, Hq, T, new_rows, max_len, causal, scale, rotary, q, out, lse, mass, mass_stride, stream):
+        return self._lib.ta_attend(ctx, C.byref(cache), Hq, T, new_rows, max_len, int(causal), C.c_float(scale), _ref(rotary), q,
+                                   out, _ptr(lse), _ptr(mass), int(mass_stride), stream)
+
+
+def _ref(structure):
+    """Reference to a structure, or None."""
+    return None if structure is None else C.byref(structure)
+
 
 def _load_call(L):
     if not os.path.exists(CALL_PATH):  # not built, or built for another Python
@@ -117,9 +152,9 @@ def _load_call(L):
         loader.exec_module(m)
     except ImportError:  # built against other system libraries
         return _CtypesCalls(L)
-    m.set_types(C.c_void_p, ta_bf16_view, ta_policy, ta_batch, ta_stream)
+    m.set_types(C.c_void_p, ta_bf16_view, ta_policy, ta_batch, ta_stream, ta_rotary, ta_cache)
     for name in ("ta_compress", "ta_compress_lse", "ta_compress_scores", "ta_stream_step", "ta_detect_embedding",
-                 "ta_sponsor_mask_conf"):
+                 "ta_sponsor_mask_conf", "ta_rotate", "ta_cache_append", "ta_cache_read", "ta_attend"):
         m.set_function(name, C.cast(getattr(L, name), C.c_void_p).value)
     return m
 
@@ -138,7 +173,8 @@ def lib():
                                     "fallback path)")
         L = C.CDLL(LIB_PATH)
         vp, i32, u64, sz = C.c_void_p, C.c_int, C.c_uint64, C.c_size_t
-        PP, PB = C.POINTER(ta_policy), C.POINTER(ta_batch)
+        PP, PB, PC, PR = C.POINTER(ta_policy), C.POINTER(ta_batch), C.POINTER(ta_cache), C.POINTER(ta_rotary)
+        f32, f64, view_t = C.c_float, C.c_double, ta_bf16_view
         sigs = {
             "ta_policy_default": (i32, [i32, i32, PP]),
             "ta_ctx_create": (i32, [i32, sz, C.POINTER(vp)]),
@@ -183,6 +219,12 @@ def lib():
             "ta_stream_scratch_bytes": (i32, [C.POINTER(ta_stream), C.POINTER(sz)]),
             "ta_stream_step": (i32, [vp, vp, PP, C.POINTER(ta_stream), vp, vp, vp, vp]),
             "ta_ctx_selftest_step_wait": (i32, [vp, vp, PP, C.POINTER(ta_stream), vp, vp, vp, u64, vp]),
+            "ta_rotary_table": (i32, [i32, f64, i32, f64, f64, f64, f64, vp, C.POINTER(f32)]),
+            "ta_rotate": (i32, [vp, PB, i32, i32, i32, PR, view_t, view_t, view_t, view_t, vp]),
+            "ta_cache_append": (i32, [vp, PC, PB, PR, view_t, view_t, vp, vp]),
+            "ta_cache_read": (i32, [vp, PC, PB, vp, view_t, view_t, vp]),
+            "ta_attend_scratch_bytes": (i32, [PC, i32, i32, i32, i32, C.POINTER(sz)]),
+            "ta_attend": (i32, [vp, PC, i32, i32, i32, i32, i32, f32, PR, view_t, view_t, vp, vp, C.c_int64, vp]),
             "ta_compress_host_workspace_bytes": (i32, [PB, i32, i32, i32, i32, PP, C.POINTER(sz)]),
             "ta_compress_host": (i32, [vp, vp, PP, PB, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
         }
@@ -424,6 +466,71 @@ def ta_stream_step(ctx, pats, policy, st: ta_stream, new_ids, attn, evicted_pos,
 def ta_ctx_selftest_step_wait(ctx, pats, policy, st: ta_stream, new_ids, attn, evicted_pos, limit_ns: int, stream=None):
     _check(lib().ta_ctx_selftest_step_wait(ctx, pats, C.byref(policy), C.byref(st), _ptr(new_ids), _ptr(attn),
                                            _ptr(evicted_pos), int(limit_ns), stream), "ta_ctx_selftest_step_wait")
+
+
+def ta_rotary_table(d_rot, base, scaling, factor, original_len, low, high, phase) -> float:
+    """Fills phase (host, d_rot // 2 64-bit integers: a numpy array or a CPU tensor) and returns the factor on rotated values."""
+    out = C.c_float(0.0)
+    _check(lib().ta_rotary_table(d_rot, base, scaling, factor, original_len, low, high, _ptr(phase), C.byref(out)),
+           "ta_rotary_table")
+    return out.value
+
+
+def make_rotary(phase, d_rot, layout=TA_ROTARY_HALF, magnitude=1.0, inverse=False, positions=None) -> ta_rotary:
+    """ta_rotary over a device copy of ta_rotary_table's phases. The tensors must outlive it."""
+    return ta_rotary(_ptr(phase), _ptr(positions), d_rot, layout, 1 if inverse else 0, magnitude)
+
+
+def ta_rotate(ctx, batch, Hq, Hkv, d, rotary: ta_rotary, q: ta_bf16_view, q_out: ta_bf16_view, k: ta_bf16_view,
+              k_out: ta_bf16_view, stream=None):
+    _check((_call or _native()).ta_rotate(ctx, batch, Hq, Hkv, d, rotary, q, q_out, k, k_out, stream), "ta_rotate")
+
+
+_FORMATS = {"torch.bfloat16": TA_CACHE_BF16, "torch.float8_e4m3fn": TA_CACHE_E4M3, "torch.int8": TA_CACHE_INT8}
+
+
+def make_cache(k, v, k_scale=None, v_scale=None, table=None, batch=None, lens=None, len_uniform=0) -> ta_cache:
+    """ta_cache over tensors k and v [L, pages, Hkv, page, d] (bfloat16, float8_e4m3fn or int8, any strides with d contiguous,
+    the same for both) with scales [L, pages, Hkv, page] for the 8-bit types. table [B, pages_per_seq] int32, or None: every
+    sequence owns pages / batch pages in a row. lens [B] or [L, B, Hkv] int32, or None: len_uniform. The tensors must outlive it."""
+    assert str(k.dtype) in _FORMATS and k.dtype == v.dtype, "keys and values are bfloat16, float8_e4m3fn or int8 alike"
+    assert k.dim() == 5 and k.shape == v.shape and k.stride() == v.stride() and k.stride(4) == 1, "k and v must be laid out alike"
+    L, pages, Hkv, page, d = k.shape
+    scales = (0, 0, 0, 0)
+    if k_scale is not None:
+        assert tuple(k_scale.shape) == (L, pages, Hkv, page) == tuple(v_scale.shape) and k_scale.stride() == v_scale.stride()
+        scales = k_scale.stride()
+    if table is not None:
+        assert table.dim() == 2 and table.stride(1) == 1 and (table.shape[0] == 1 or table.stride(0) == table.shape[1])
+        batch, wide = table.shape
+    else:
+        assert batch and pages % batch == 0, "without a table every sequence has the same number of pages"
+        wide = pages // batch
+    per_unit = lens is not None and lens.dim() > 1
+    assert lens is None or (lens.is_contiguous() and tuple(lens.shape) == ((L, batch, Hkv) if per_unit else (batch,)))
+    return ta_cache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), *k.stride()[:4], *scales, _ptr(table), _ptr(lens), L, batch, Hkv,
+                    d, _FORMATS[str(k.dtype)], page, pages, wide, 1 if per_unit else 0, len_uniform)
+
+
+def ta_cache_append(ctx, cache: ta_cache, batch, rotary, k: ta_bf16_view, v: ta_bf16_view, rows=None, stream=None):
+    _check((_call or _native()).ta_cache_append(ctx, cache, batch, rotary, k, v, rows, stream), "ta_cache_append")
+
+
+def ta_cache_read(ctx, cache: ta_cache, batch, rows, k_out: ta_bf16_view, v_out: ta_bf16_view, stream=None):
+    _check((_call or _native()).ta_cache_read(ctx, cache, batch, rows, k_out, v_out, stream), "ta_cache_read")
+
+
+def ta_attend_scratch_bytes(cache: ta_cache, Hq, T, max_len, with_mass=False) -> int:
+    out = C.c_size_t(0)
+    _check(lib().ta_attend_scratch_bytes(C.byref(cache), Hq, T, max_len, 1 if with_mass else 0, C.byref(out)),
+           "ta_attend_scratch_bytes")
+    return out.value
+
+
+def ta_attend(ctx, cache: ta_cache, Hq, T, new_rows, max_len, causal, scale, rotary, q: ta_bf16_view, out: ta_bf16_view, lse=None,
+              mass=None, mass_stride=0, stream=None):
+    _check((_call or _native()).ta_attend(ctx, cache, Hq, T, new_rows, max_len, causal, scale, rotary, q, out, lse, mass,
+                                          mass_stride, stream), "ta_attend")
 
 
 def ta_compress_host_workspace_bytes(batch, Hq, Hkv, d, K, policy) -> int:

@@ -16,12 +16,14 @@ PyObject* g_view = nullptr;         // the ctypes structures of the binding
 PyObject* g_policy = nullptr;
 PyObject* g_batch = nullptr;
 PyObject* g_stream = nullptr;
+PyObject* g_rotary = nullptr;
+PyObject* g_cache = nullptr;
 PyObject* g_data_ptr = nullptr;     // interned names
 PyObject* g_stride = nullptr;
 PyObject* g_ctypes = nullptr;
 PyObject* g_data = nullptr;
 
-enum Fn { kCompress, kCompressLse, kCompressScores, kStreamStep, kDetect, kMaskConf, kFns };
+enum Fn { kCompress, kCompressLse, kCompressScores, kStreamStep, kDetect, kMaskConf, kRotate, kCacheAppend, kCacheRead, kAttend, kFns };
 void* g_fn[kFns];
 
 // The memory of a ctypes object of type `cls`. The object outlives the call: the caller's argument list holds it.
@@ -89,6 +91,12 @@ struct Args {  // reads the arguments in order; `ok` turns false with a Python e
     if (ok) ok = ctypes_memory(*v, cls, sizeof(T), &p);
     ++v;
     return static_cast<T*>(p);
+  }
+  template <class T>
+  T* object_or_none(PyObject* cls) {
+    if (*v != Py_None) return object<T>(cls);
+    ++v;
+    return nullptr;
   }
   ta_bf16_view view() {
     ta_bf16_view r = {};
@@ -251,6 +259,67 @@ PyObject* mask_conf(PyObject*, PyObject* const* v, Py_ssize_t n) {
   });
 }
 
+PyObject* rotate(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (!count_is(n, 11)) return nullptr;
+  Args a{v};
+  auto* ctx = a.ptr<ta_ctx>();
+  auto* batch = a.object<ta_batch>(g_batch);
+  const int Hq = (int)a.num(), Hkv = (int)a.num(), d = (int)a.num();
+  auto* rot = a.object_or_none<ta_rotary>(g_rotary);
+  const ta_bf16_view q = a.view(), qo = a.view(), k = a.view(), ko = a.view();
+  auto* st = a.ptr<void>();
+  return run(a.ok, [&] {
+    return reinterpret_cast<decltype(&ta_rotate)>(g_fn[kRotate])(ctx, batch, Hq, Hkv, d, rot, q, qo, k, ko, st);
+  });
+}
+
+PyObject* cache_append(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (!count_is(n, 8)) return nullptr;
+  Args a{v};
+  auto* ctx = a.ptr<ta_ctx>();
+  auto* cache = a.object<ta_cache>(g_cache);
+  auto* batch = a.object<ta_batch>(g_batch);
+  auto* rot = a.object_or_none<ta_rotary>(g_rotary);
+  const ta_bf16_view k = a.view(), vv = a.view();
+  auto* rows = a.ptr<int32_t>();
+  auto* st = a.ptr<void>();
+  return run(a.ok, [&] {
+    return reinterpret_cast<decltype(&ta_cache_append)>(g_fn[kCacheAppend])(ctx, cache, batch, rot, k, vv, rows, st);
+  });
+}
+
+PyObject* cache_read(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (!count_is(n, 7)) return nullptr;
+  Args a{v};
+  auto* ctx = a.ptr<ta_ctx>();
+  auto* cache = a.object<ta_cache>(g_cache);
+  auto* batch = a.object<ta_batch>(g_batch);
+  auto* rows = a.ptr<int32_t>();
+  const ta_bf16_view k = a.view(), vv = a.view();
+  auto* st = a.ptr<void>();
+  return run(a.ok, [&] {
+    return reinterpret_cast<decltype(&ta_cache_read)>(g_fn[kCacheRead])(ctx, cache, batch, rows, k, vv, st);
+  });
+}
+
+PyObject* attend(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (!count_is(n, 15)) return nullptr;
+  Args a{v};
+  auto* ctx = a.ptr<ta_ctx>();
+  auto* cache = a.object<ta_cache>(g_cache);
+  const int Hq = (int)a.num(), T = (int)a.num(), new_rows = (int)a.num(), max_len = (int)a.num(), causal = (int)a.num();
+  const float scale = a.real();
+  auto* rot = a.object_or_none<ta_rotary>(g_rotary);
+  const ta_bf16_view q = a.view(), out = a.view();
+  auto *lse = a.ptr<float>(), *mass = a.ptr<float>();
+  const int64_t mass_stride = a.num();
+  auto* st = a.ptr<void>();
+  return run(a.ok, [&] {
+    return reinterpret_cast<decltype(&ta_attend)>(g_fn[kAttend])(ctx, cache, Hq, T, new_rows, max_len, causal, scale, rot, q, out,
+                                                                lse, mass, mass_stride, st);
+  });
+}
+
 // view(tensor, ragged): strides and address of a [L, B, H, n, d] or ragged [L, H, total, d] tensor as a ta_bf16_view
 PyObject* view(PyObject*, PyObject* const* v, Py_ssize_t n) {
   if (!count_is(n, 2)) return nullptr;
@@ -291,9 +360,9 @@ PyObject* view(PyObject*, PyObject* const* v, Py_ssize_t n) {
 }
 
 PyObject* set_types(PyObject*, PyObject* const* v, Py_ssize_t n) {
-  if (!count_is(n, 5)) return nullptr;
-  PyObject** to[5] = {&g_void_p, &g_view, &g_policy, &g_batch, &g_stream};
-  for (int i = 0; i < 5; ++i) {
+  if (!count_is(n, 7)) return nullptr;
+  PyObject** to[7] = {&g_void_p, &g_view, &g_policy, &g_batch, &g_stream, &g_rotary, &g_cache};
+  for (int i = 0; i < 7; ++i) {
     if (!PyType_Check(v[i])) {
       PyErr_SetString(PyExc_TypeError, "types are needed");
       return nullptr;
@@ -308,7 +377,8 @@ PyObject* set_types(PyObject*, PyObject* const* v, Py_ssize_t n) {
 PyObject* set_function(PyObject*, PyObject* const* v, Py_ssize_t n) {
   if (!count_is(n, 2)) return nullptr;
   static const char* names[kFns] = {"ta_compress", "ta_compress_lse", "ta_compress_scores", "ta_stream_step",
-                                    "ta_detect_embedding", "ta_sponsor_mask_conf"};
+                                    "ta_detect_embedding", "ta_sponsor_mask_conf", "ta_rotate", "ta_cache_append",
+                                    "ta_cache_read", "ta_attend"};
   const char* name = PyUnicode_AsUTF8(v[0]);
   if (!name) return nullptr;
   for (int i = 0; i < kFns; ++i)
@@ -322,7 +392,7 @@ PyObject* set_function(PyObject*, PyObject* const* v, Py_ssize_t n) {
 
 #define TA_METHOD(name, f, doc) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL, doc}
 PyMethodDef methods[] = {
-    TA_METHOD("set_types", set_types, "c_void_p and the structures view, policy, batch, stream"),
+    TA_METHOD("set_types", set_types, "c_void_p and the structures view, policy, batch, stream, rotary, cache"),
     TA_METHOD("set_function", set_function, "name and address of an entry point"),
     TA_METHOD("view", view, "ta_bf16_view of a tensor"),
     TA_METHOD("ta_compress", compress, "status of the call"),
@@ -331,6 +401,10 @@ PyMethodDef methods[] = {
     TA_METHOD("ta_stream_step", stream_step, "status of the call"),
     TA_METHOD("ta_detect_embedding", detect, "status of the call"),
     TA_METHOD("ta_sponsor_mask_conf", mask_conf, "status of the call"),
+    TA_METHOD("ta_rotate", rotate, "status of the call"),
+    TA_METHOD("ta_cache_append", cache_append, "status of the call"),
+    TA_METHOD("ta_cache_read", cache_read, "status of the call"),
+    TA_METHOD("ta_attend", attend, "status of the call"),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ta_call", "argument marshalling for libta.so", -1, methods, nullptr, nullptr,
                       nullptr, nullptr};

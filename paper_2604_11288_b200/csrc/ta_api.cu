@@ -1,12 +1,13 @@
 // Host side of libta.so: argument validation, scratch carving and launch sequencing for the entry points declared
 // in ta.h. Nothing here computes any part of the method; every step runs in the kernels of ta_mask.cu, ta_score.cu,
-// ta_select.cu and ta_compact.cu.
+// ta_select.cu and ta_compact.cu, and those of the decode loop's operators in ta_rotate.cu, ta_cache.cu and ta_attend.cu.
 #include <cuda.h>
 #include <math.h>
 #include <nvtx3/nvToolsExt.h>
 #include <new>
 #include <string.h>
 
+#include "ta_cache.cuh"
 #include "ta_internal.cuh"
 
 namespace {
@@ -95,7 +96,7 @@ ta_status check_heads(int Hq, int Hkv, int d, const ta_policy* p, bool scored) {
   return TA_OK;
 }
 
-ta_status check_view(const ta_bf16_view& v, bool need_b) {
+ta_status check_view(const ta_bf16_view& v, bool need_b, int d = TA_HEAD_DIM) {
   if (!v.ptr) return TA_ERR_INVALID_ARG;
   if ((uintptr_t)v.ptr % 16) return TA_ERR_ALIGNMENT;
   const int64_t s[4] = {v.stride_l, v.stride_b, v.stride_h, v.stride_n};
@@ -104,7 +105,7 @@ ta_status check_view(const ta_bf16_view& v, bool need_b) {
     if (s[i] < 0) return TA_ERR_INVALID_ARG;
     if (s[i] % 8) return TA_ERR_ALIGNMENT;
   }
-  if (v.stride_n < TA_HEAD_DIM) return TA_ERR_INVALID_ARG;
+  if (v.stride_n < d) return TA_ERR_INVALID_ARG;
   return TA_OK;
 }
 
@@ -1063,6 +1064,234 @@ ta_status ta_ctx_selftest_step_wait(ta_ctx* ctx, const ta_patterns* pats, const 
                                     void* stream) {
   if (limit_ns == 0 || limit_ns > 1000000000ull) return TA_ERR_INVALID_ARG;
   return stream_step_impl(ctx, pats, policy, st, new_ids, attn, evicted_pos, limit_ns, stream);
+}
+
+// ---------------------------------------------------------------------------------------------- the decode loop's operators
+namespace {
+ta_status check_cache(const ta_cache* c) {
+  if (!c || !c->k || !c->v) return TA_ERR_INVALID_ARG;
+  if (c->format < TA_CACHE_BF16 || c->format > TA_CACHE_INT8) return TA_ERR_INVALID_ARG;
+  if (c->n_layers < 1 || c->batch < 1 || c->Hkv < 1 || c->page < 1 || c->n_pages < 1 || c->pages_per_seq < 1) return TA_ERR_INVALID_ARG;
+  if (c->d != 64 && c->d != 128) return TA_ERR_UNSUPPORTED;
+  if ((long long)c->n_layers * c->batch * c->Hkv > 0x7fffffffLL || c->n_layers > 65535) return TA_ERR_UNSUPPORTED;
+  const bool codes = c->format != TA_CACHE_BF16;
+  if (codes && (!c->k_scale || !c->v_scale)) return TA_ERR_INVALID_ARG;
+  if ((uintptr_t)c->k % 16 || (uintptr_t)c->v % 16) return TA_ERR_ALIGNMENT;
+  const int64_t s[4] = {c->stride_l, c->stride_p, c->stride_h, c->stride_r};
+  for (int64_t x : s) {
+    if (x < 0) return TA_ERR_INVALID_ARG;
+    if (x % (codes ? 16 : 8)) return TA_ERR_ALIGNMENT;
+  }
+  if (c->page > 1 && c->stride_r < c->d) return TA_ERR_INVALID_ARG;
+  if (codes && (c->scale_stride_l < 0 || c->scale_stride_p < 0 || c->scale_stride_h < 0 || c->scale_stride_r < 0))
+    return TA_ERR_INVALID_ARG;
+  if (!c->lens && c->len_uniform < 0) return TA_ERR_INVALID_ARG;
+  return TA_OK;
+}
+ta_cache_dev cache_dev(const ta_cache& c) {
+  ta_cache_dev d = {};
+  const int64_t bytes = c.format == TA_CACHE_BF16 ? 2 : 1;
+  d.k = static_cast<uint8_t*>(c.k);
+  d.v = static_cast<uint8_t*>(c.v);
+  d.ks = c.k_scale;
+  d.vs = c.v_scale;
+  d.sl = c.stride_l * bytes;
+  d.sp = c.stride_p * bytes;
+  d.sh = c.stride_h * bytes;
+  d.sr = c.stride_r * bytes;
+  d.ssl = c.scale_stride_l;
+  d.ssp = c.scale_stride_p;
+  d.ssh = c.scale_stride_h;
+  d.ssr = c.scale_stride_r;
+  d.table = c.table;
+  d.lens = c.lens;
+  d.batch = c.batch;
+  d.Hkv = c.Hkv;
+  d.format = c.format;
+  d.page = c.page;
+  d.page_shift = -1;
+  for (int s = 0; s < 31; ++s)
+    if (c.page == 1 << s) d.page_shift = s;
+  d.n_pages = c.n_pages;
+  d.wide = c.pages_per_seq;
+  d.lens_per_unit = c.lens_per_unit;
+  d.len_uniform = c.len_uniform;
+  return d;
+}
+ta_status check_rotary(const ta_rotary* r, int d) {
+  if (!r || !r->phase) return TA_ERR_INVALID_ARG;
+  if (r->layout != TA_ROTARY_HALF && r->layout != TA_ROTARY_INTERLEAVED) return TA_ERR_INVALID_ARG;
+  if (!isfinite(r->magnitude)) return TA_ERR_INVALID_ARG;
+  if (r->d_rot < 2 || r->d_rot > d || r->d_rot % 2) return TA_ERR_INVALID_ARG;
+  if (r->d_rot % 8) return TA_ERR_UNSUPPORTED;
+  return TA_OK;
+}
+ta_rotary_dev rotary_dev(const ta_rotary* r) {
+  ta_rotary_dev d = {};
+  if (!r) return d;
+  d.phase = r->phase;
+  d.positions = r->positions;
+  d.d_rot = r->d_rot;
+  d.interleaved = r->layout == TA_ROTARY_INTERLEAVED;
+  d.inverse = r->inverse ? 1 : 0;
+  d.magnitude = r->magnitude;
+  return d;
+}
+ta_status check_move(const ta_ctx* ctx, const ta_cache* cache, const ta_batch* batch, const ta_bf16_view& k, const ta_bf16_view& v) {
+  if (!ctx) return TA_ERR_INVALID_ARG;
+  ta_status s = check_cache(cache);
+  if (s == TA_OK) s = check_batch(batch);
+  if (s != TA_OK) return s;
+  if (batch->n_layers != cache->n_layers || batch->batch != cache->batch) return TA_ERR_INVALID_ARG;
+  s = check_view(k, batch->cu_seqlens == nullptr, cache->d);
+  return s == TA_OK ? check_view(v, batch->cu_seqlens == nullptr, cache->d) : s;
+}
+ta_cache_move_args move_args(const ta_cache& cache, const ta_batch& batch, const ta_bf16_view& k, const ta_bf16_view& v,
+                             const int32_t* rows) {
+  ta_cache_move_args a = {};
+  a.cache = cache_dev(cache);
+  a.seq = seq_desc(batch);
+  a.n_layers = batch.n_layers;
+  a.d = cache.d;
+  a.k = k;
+  a.v = v;
+  a.rows = rows;
+  return a;
+}
+ta_status check_attend(const ta_cache* c, int Hq, int T, int max_len) {
+  ta_status s = check_cache(c);
+  if (s != TA_OK) return s;
+  if (Hq < c->Hkv || Hq % c->Hkv || T < 1 || max_len < 0) return TA_ERR_INVALID_ARG;
+  if (T > TA_MAX_NEW_TOKENS || Hq / c->Hkv > 256 || max_len > TA_MAX_SEQ_LEN) return TA_ERR_UNSUPPORTED;
+  return TA_OK;
+}
+}  // namespace
+
+ta_status ta_rotary_table(int d_rot, double base, int scaling, double factor, double original_len, double low, double high,
+                          uint64_t* phase, float* magnitude) {
+  if (!phase || !magnitude || d_rot < 2 || d_rot % 2 || !(base > 1.0) || !isfinite(base)) return TA_ERR_INVALID_ARG;
+  if (scaling < TA_SCALING_PLAIN || scaling > TA_SCALING_BAND) return TA_ERR_INVALID_ARG;
+  if (scaling != TA_SCALING_PLAIN && !(factor >= 1.0 && isfinite(factor))) return TA_ERR_INVALID_ARG;
+  const bool blend = scaling == TA_SCALING_RAMP || scaling == TA_SCALING_BAND;
+  if (blend && !(original_len > 0.0 && isfinite(original_len) && low > 0.0 && high > low && isfinite(high))) return TA_ERR_INVALID_ARG;
+  if (scaling == TA_SCALING_BASE && d_rot < 4) return TA_ERR_INVALID_ARG;
+  const double two_pi = 6.283185307179586476925;
+  const double b = scaling == TA_SCALING_BASE ? base * pow(factor, (double)d_rot / (d_rot - 2)) : base;
+  double first = 0.0, last = 0.0;  // TA_SCALING_RAMP: the pairs between which the share of the plain frequency falls from 1 to 0
+  if (scaling == TA_SCALING_RAMP) {
+    const double pairs_per_e = d_rot / (2.0 * log(base));
+    first = fmax(floor(pairs_per_e * log(original_len / (high * two_pi))), 0.0);
+    last = fmin(ceil(pairs_per_e * log(original_len / (low * two_pi))), d_rot - 1.0);
+  }
+  for (int i = 0; i < d_rot / 2; ++i) {
+    double f = pow(b, -2.0 * i / d_rot);
+    double plain = scaling == TA_SCALING_LINEAR ? 0.0 : 1.0;
+    if (scaling == TA_SCALING_RAMP) plain = 1.0 - fmin(fmax((i - first) / fmax(last - first, 0.001), 0.0), 1.0);
+    if (scaling == TA_SCALING_BAND) plain = fmin(fmax((original_len * f / two_pi - low) / (high - low), 0.0), 1.0);
+    if (plain < 1.0) f = f / factor * (1.0 - plain) + f * plain;
+    phase[i] = (uint64_t)(f / two_pi * 0x1p64);  // under one turn: frequencies are at most 1 radian per position
+  }
+  *magnitude = scaling == TA_SCALING_RAMP ? (float)(0.1 * log(factor) + 1.0) : 1.0f;
+  return TA_OK;
+}
+
+ta_status ta_rotate(ta_ctx* ctx, const ta_batch* batch, int Hq, int Hkv, int d, const ta_rotary* rotary, ta_bf16_view q,
+                    ta_bf16_view q_out, ta_bf16_view k, ta_bf16_view k_out, void* stream) {
+  Range range("ta_rotate");
+  if (!ctx || Hq < 1 || Hkv < 0 || d < 8) return TA_ERR_INVALID_ARG;
+  ta_status s = check_batch(batch);
+  if (s != TA_OK) return s;
+  if (d % 8 || d > TA_MAX_ROTATE_DIM || batch->n_layers > 65535 || Hq + (long long)Hkv > 4096) return TA_ERR_UNSUPPORTED;
+  s = check_rotary(rotary, d);
+  const bool uniform = batch->cu_seqlens == nullptr;
+  const ta_bf16_view* views[4] = {&q, &q_out, &k, &k_out};
+  for (int i = 0; i < (Hkv ? 4 : 2) && s == TA_OK; ++i) s = check_view(*views[i], uniform, d);
+  if (s != TA_OK) return s;
+  DeviceGuard guard(ctx->device);
+  ta_rotate_args a = {};
+  a.seq = seq_desc(*batch);
+  a.n_layers = batch->n_layers;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.d = d;
+  a.rot = rotary_dev(rotary);
+  a.q = q;
+  a.q_out = q_out;
+  a.k = k;
+  a.k_out = k_out;
+  cudaError_t e = ta_launch_rotate(a, (cudaStream_t)stream);
+  return e == cudaSuccess ? TA_OK : cuda_fail(ctx, e);
+}
+
+ta_status ta_cache_append(ta_ctx* ctx, const ta_cache* cache, const ta_batch* batch, const ta_rotary* rotary, ta_bf16_view k,
+                          ta_bf16_view v, const int32_t* rows, void* stream) {
+  Range range("ta_cache_append");
+  ta_status s = check_move(ctx, cache, batch, k, v);
+  if (s == TA_OK && rotary) s = check_rotary(rotary, cache->d);
+  if (s != TA_OK) return s;
+  DeviceGuard guard(ctx->device);
+  ta_cache_move_args a = move_args(*cache, *batch, k, v, rows);
+  a.rot = rotary_dev(rotary);
+  cudaError_t e = ta_launch_cache_append(a, ctx->d_status, (cudaStream_t)stream);
+  return e == cudaSuccess ? TA_OK : cuda_fail(ctx, e);
+}
+
+ta_status ta_cache_read(ta_ctx* ctx, const ta_cache* cache, const ta_batch* batch, const int32_t* rows, ta_bf16_view k_out,
+                        ta_bf16_view v_out, void* stream) {
+  Range range("ta_cache_read");
+  ta_status s = check_move(ctx, cache, batch, k_out, v_out);
+  if (s != TA_OK) return s;
+  DeviceGuard guard(ctx->device);
+  const ta_cache_move_args a = move_args(*cache, *batch, k_out, v_out, rows);
+  cudaError_t e = ta_launch_cache_read(a, ctx->d_status, (cudaStream_t)stream);
+  return e == cudaSuccess ? TA_OK : cuda_fail(ctx, e);
+}
+
+ta_status ta_attend_scratch_bytes(const ta_cache* cache, int Hq, int T, int max_len, int with_mass, size_t* out_bytes) {
+  if (!out_bytes) return TA_ERR_INVALID_ARG;
+  ta_status s = check_attend(cache, Hq, T, max_len);
+  if (s != TA_OK) return s;
+  *out_bytes = align_up(ta_attend_scratch(cache->n_layers * cache->batch * cache->Hkv, Hq / cache->Hkv * T, cache->d, max_len,
+                                          with_mass != 0)) +
+               kAlign;
+  return TA_OK;
+}
+
+ta_status ta_attend(ta_ctx* ctx, const ta_cache* cache, int Hq, int T, int new_rows, int max_len, int causal, float scale,
+                    const ta_rotary* rotary, ta_bf16_view q, ta_bf16_view out, float* lse, float* mass, int64_t mass_stride,
+                    void* stream) {
+  Range range("ta_attend");
+  if (!ctx) return TA_ERR_INVALID_ARG;
+  ta_status s = check_attend(cache, Hq, T, max_len);
+  if (s == TA_OK && rotary) s = check_rotary(rotary, cache->d);
+  if (s == TA_OK) s = check_view(q, true, cache->d);
+  if (s == TA_OK) s = check_view(out, true, cache->d);
+  if (s != TA_OK) return s;
+  if (new_rows < 0 || !(scale >= 0.0f) || !isfinite(scale) || (mass && mass_stride < max_len)) return TA_ERR_INVALID_ARG;
+  const int units = cache->n_layers * cache->batch * cache->Hkv;
+  if (ta_attend_scratch(units, Hq / cache->Hkv * T, cache->d, max_len, mass != nullptr) > ctx->scratch_bytes)
+    return TA_ERR_SCRATCH_TOO_SMALL;
+  DeviceGuard guard(ctx->device);
+  ctx->cached_epoch = 0;
+  ta_attend_args a = {};
+  a.cache = cache_dev(*cache);
+  a.n_layers = cache->n_layers;
+  a.Hq = Hq;
+  a.d = cache->d;
+  a.T = T;
+  a.new_rows = new_rows;
+  a.max_len = max_len;
+  a.causal = causal ? 1 : 0;
+  a.scale = scale > 0.0f ? scale : (float)(1.0 / sqrt((double)cache->d));
+  a.rot = rotary_dev(rotary);
+  a.q = q;
+  a.out = out;
+  a.lse = lse;
+  a.mass = mass;
+  a.mass_stride = mass_stride;
+  a.scratch = ctx->scratch;
+  cudaError_t e = ta_launch_attend(a, ctx->d_status, (cudaStream_t)stream);
+  return e == cudaSuccess ? TA_OK : cuda_fail(ctx, e);
 }
 
 // ---------------------------------------------------------------------------------------------- host buffers
