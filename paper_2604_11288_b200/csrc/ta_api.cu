@@ -226,10 +226,12 @@ ta_status ta_ctx_create(int device, size_t scratch_bytes, ta_ctx** out) {
   c->device = device;
   c->sm_count = prop.multiProcessorCount;
   c->scratch_bytes = scratch_bytes;
-  // the status block and, behind it, the decode step's words
-  constexpr size_t kWords = 256, kSyncBytes = kWords + kStreamWords * sizeof(ulonglong2);
+  // the status block and, behind it, the decode step's words and the attention's tickets
+  constexpr size_t kWords = 256, kTickets = kWords + kStreamWords * sizeof(ulonglong2),
+                   kSyncBytes = kTickets + kAttendTickets * sizeof(int);
   cudaError_t e = cudaMalloc(&c->d_status, kSyncBytes);
   c->stream_sync.words = reinterpret_cast<ulonglong2*>(reinterpret_cast<uint8_t*>(c->d_status) + kWords);
+  c->attend_tickets = reinterpret_cast<int*>(reinterpret_cast<uint8_t*>(c->d_status) + kTickets);
   if (e == cudaSuccess && scratch_bytes) e = cudaMalloc(&c->scratch, scratch_bytes);
   for (int i = 0; e == cudaSuccess && i < 8; ++i) e = cudaEventCreate(&c->ev[i]);
   if (e == cudaSuccess) e = cudaStreamCreateWithFlags(&c->copy_in, cudaStreamNonBlocking);
@@ -1290,7 +1292,7 @@ ta_status ta_attend(ta_ctx* ctx, const ta_cache* cache, int Hq, int T, int new_r
   a.mass = mass;
   a.mass_stride = mass_stride;
   a.scratch = ctx->scratch;
-  cudaError_t e = ta_launch_attend(a, ctx->d_status, (cudaStream_t)stream);
+  cudaError_t e = ta_launch_attend(a, ctx->attend_tickets, ctx->d_status, (cudaStream_t)stream);
   return e == cudaSuccess ? TA_OK : cuda_fail(ctx, e);
 }
 

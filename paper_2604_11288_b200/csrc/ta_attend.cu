@@ -1,143 +1,843 @@
 // Attention of new tokens over a cache.
+//
+// A unit (layer, sequence, KV head) has R = (Hq / Hkv) * T query rows that read the same n cache rows, each once: 4 d R
+// operations for 4 d bytes (bf16), so up to some tens of query rows the cache's bytes are the bound, and everything below
+// serves to keep them coming. The cache rows of a unit are cut into pieces of `piece` rows, a block each; a block's four
+// warps take its tiles (16 or 32 rows) in turn, each with a ring of its own in shared memory that asynchronous 16-byte
+// copies fill two tiles ahead, so no warp waits for another before the end. Any page size and any strides: a lane looks up
+// one row of the next tile one tile early. Rows that are not there are filled with zeros and masked.
+//
+// Per tile and warp: scores S = Q K^T on the tensor cores (m16n8k16, fp32 sums), a running maximum and sum per query row,
+// O = O + P V on the tensor cores with P straight from the score registers. Products have 8 to 32 rows: far too few for a
+// tcgen05 tile of 128 to pay, and what moves the data is the same. The order of the d coordinates inside a product is free as
+// long as both operands use the same one: a lane's 16 bytes of a key row serve as its fragments of two (bf16) or four (8-bit)
+// products without a shuffle.
+//
+// Precision. bf16 caches: products of bf16 values. 8-bit caches: codes are exact in fp16; queries are scaled per row by a power
+// of two into fp16's range (and back in the score's factor), the scale of a key row multiplies its scores, that of a value row
+// its probabilities, relative to the largest power of two among the scales so far. Probabilities and rotated queries
+// enter their products as a sum of two 16-bit parts, hi + lo: with up to 8 query rows the lower half of the 16-row product,
+// which would be empty, holds the lo parts at no cost (MB = 0); with more rows the lo parts are a second product.
+#include <cuda_fp16.h>
 #include <math.h>
 
 #include "ta_cache.cuh"
+#include "ta_sm100.cuh"
 
 namespace {
 
+using ta_sm100::ex2;
+using ta_sm100::smem_u32;
+
 constexpr int kWarps = 4;
+constexpr int kThreads = kWarps * 32;
+constexpr int kStages = 3;
 
-__device__ __forceinline__ float cache_value(const ta_cache_dev& c, const uint8_t* row, int j) {
-  if (c.format == TA_CACHE_BF16) return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(row)[j]);
-  if (c.format == TA_CACHE_E4M3) return __half2float(__half(__nv_cvt_fp8_to_halfraw(row[j], __NV_E4M3)));
-  return (float)reinterpret_cast<const int8_t*>(row)[j];
+template <int D, int FMT>
+struct Shape {
+  static constexpr bool CODES = FMT != TA_CACHE_BF16;
+  static constexpr int ROW = D * (CODES ? 1 : 2);                 // bytes of a row
+  static constexpr int CHUNKS = ROW / 16;
+  static constexpr int TK = (CODES || D == 64) ? 32 : 16;         // cache rows of a tile
+  static constexpr int TILE = TK * ROW;                           // bytes of K, and of V, in a stage
+  static constexpr int STAGE = 2 * TILE + (CODES ? 2 * TK * 4 : 0);
+  static constexpr int KS = D / 16;                               // products along d
+  static constexpr int RING = kWarps * kStages * STAGE;
+};
+__host__ __device__ constexpr int rows_of(int MB) { return MB == 0 ? 8 : 16 * MB; }  // query rows of a block
+template <int D, int FMT, int MB>
+constexpr int smem_bytes() {
+  constexpr int R = rows_of(MB);
+  constexpr int q32 = R * D * 4;                             // queries in fp32
+  constexpr int frag = MB == 0 ? 0 : 2 * MB * (D / 16) * 512;  // their fragments, hi and lo
+  constexpr int join = kWarps * R * (D + 4) * 4;
+  constexpr int ring = Shape<D, FMT>::RING > join ? Shape<D, FMT>::RING : join;
+  return ring + q32 + frag + R * 8 /* row factor, limit */ + kWarps * R * 8 /* m, l */ + kWarps * kStages * 4 + 16;
 }
 
-// A block per query row: its warps take every kWarps-th cache row each, with a running maximum and sum, and join at the end.
-// grid.x = units, grid.y = rows of a unit. scores: [unit][row][max_len] for the attention mass, or null.
-template <int D>
-__global__ void __launch_bounds__(kWarps * 32) ta_attend_kernel(ta_attend_args a, float* scores, float* row_lse,
-                                                                 ta_dev_status* status) {
-  ta_wait_for_prior_grid();
-  constexpr int N = D / 32;
-  __shared__ float s_q[D], s_m[kWarps], s_l[kWarps], s_o[kWarps][D];
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp4(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ float2 lds_f2(uint32_t a) {
+  const uint2 v = lds64(a);
+  return make_float2(__uint_as_float(v.x), __uint_as_float(v.y));
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(a));
+}
+template <bool CODES>  // fp16 operands for 8-bit caches, bf16 otherwise
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (CODES)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// x and y as a pair of 16-bit values (x in the lower half), and what the rounding left
+template <bool CODES>
+__device__ __forceinline__ uint32_t pack2(float x, float y) {
+  uint32_t r;
+  if constexpr (CODES) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
+  else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
+  return r;
+}
+template <bool CODES>
+__device__ __forceinline__ float2 unpack2(uint32_t p) {
+  if constexpr (CODES) return __half22float2(*reinterpret_cast<__half2*>(&p));
+  else return make_float2(__uint_as_float(p << 16), __uint_as_float(p & 0xffff0000u));
+}
+template <bool CODES>
+__device__ __forceinline__ uint32_t rest2(float x, float y, uint32_t hi) {
+  const float2 h = unpack2<CODES>(hi);
+  return pack2<CODES>(x - h.x, y - h.y);
+}
+// four codes as two pairs of fp16, exactly
+template <int FMT>
+__device__ __forceinline__ void expand(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  if constexpr (FMT == TA_CACHE_E4M3) {
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+        : "=r"(lo), "=r"(hi)
+        : "r"(w));
+  } else {  // c + 128 in the mantissa of 1024, less 1152
+    const uint32_t u = w ^ 0x80808080u;
+    const uint32_t a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
+    const __half2 off = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));
+    const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&a), off), y = __hsub2(*reinterpret_cast<const __half2*>(&b), off);
+    lo = *reinterpret_cast<const uint32_t*>(&x);
+    hi = *reinterpret_cast<const uint32_t*>(&y);
+  }
+}
+__device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }  // -126 <= e <= 127
+
+struct Unit {
+  int l, b, g, n;  // n: rows that are there
+};
+__device__ __forceinline__ Unit unit_of(const ta_attend_args& a, int unit, bool report, ta_dev_status* status) {
   const ta_cache_dev& c = a.cache;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int unit = blockIdx.x, g = unit % c.Hkv, b = unit / c.Hkv % c.batch, l = unit / c.Hkv / c.batch;
-  const int G = a.Hq / c.Hkv, t = blockIdx.y / G, h = g * G + blockIdx.y % G;
-  long long n = (long long)ta_cache_len(c, l, b, g) + a.new_rows;
+  Unit u;
+  u.g = unit % c.Hkv;
+  const int lb = unit / c.Hkv;
+  u.b = lb % c.batch;
+  u.l = lb / c.batch;
+  const long long asked = (long long)ta_cache_len(c, u.l, u.b, u.g) + a.new_rows;
   const long long most = min((long long)a.max_len, (long long)c.wide * c.page);
-  if (n > most) {
-    if (threadIdx.x == 0) ta_report_bounds(status, 32, b, (int)min(n, 0x7fffffffLL));
-    n = most;
-  }
-  const int seen = (int)max(0LL, n - (a.causal ? a.T - 1 - t : 0));
-  const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(a.q.ptr) + l * a.q.stride_l + b * a.q.stride_b + h * a.q.stride_h +
-                           t * a.q.stride_n;
-  for (int j = threadIdx.x; j < D; j += kWarps * 32) {
-    float v = __bfloat162float(q[j]);
-    if (a.rot.phase && j < a.rot.d_rot) {
-      const int half = a.rot.d_rot / 2;
-      const int position = a.rot.positions ? a.rot.positions[b * a.T + t] : (int)n - a.T + t;
-      const bool second = a.rot.interleaved ? (j & 1) : j >= half;
-      const int p = a.rot.interleaved ? j >> 1 : (second ? j - half : j);
-      const int other = a.rot.interleaved ? j ^ 1 : (second ? j - half : j + half);
-      const float2 cs = ta_cos_sin(a.rot, a.rot.phase[p], position);
-      const float o = __bfloat162float(q[other]);
-      v = second ? o * cs.y + v * cs.x : v * cs.x - o * cs.y;
+  if (asked > most && report) ta_report_bounds(status, 32, u.b, (int)min(asked, 0x7fffffffLL));
+  u.n = (int)max(0LL, min(asked, most));
+  return u;
+}
+
+struct Scratch {    // of one call (null: not used)
+  float* part;      // [unit][row block][piece][row][D], unnormalised
+  float2* part_ml;  // [unit][row block][piece][row]: maximum (in bits) and sum
+  int* ticket;      // [unit][row block], zero between calls
+  float* score;     // [unit][row][score_stride], in bits
+  float2* row_ml;   // [unit][row]: maximum and 1 / sum for the attention mass
+  long long score_stride;
+};
+
+__device__ __forceinline__ float joined_max(const float2* ml, int parts, long long stride) {
+  float m = -INFINITY;
+  for (int i = 0; i < parts; ++i) m = fmaxf(m, __ldcg(&ml[i * stride].x));
+  return m;
+}
+
+// blockIdx.x = (unit * row blocks + block) * pieces + piece
+template <int D, int FMT, int MB>
+__global__ void __launch_bounds__(kThreads) ta_attend_kernel(ta_attend_args a, Scratch sc, int pieces, int piece, int row_blocks,
+                                                              ta_dev_status* status) {
+  using S = Shape<D, FMT>;
+  constexpr bool CODES = S::CODES, NARROW = MB == 0;
+  constexpr int TK = S::TK, NT = TK / 8, KS = S::KS, R = rows_of(MB), MBN = NARROW ? 1 : MB, NR = NARROW ? 1 : 2 * MB;
+  constexpr int NJ = D / 8;  // 8-wide tiles of the output
+  extern __shared__ __align__(128) uint8_t smem[];
+  constexpr int join_bytes = kWarps * R * (D + 4) * 4;
+  uint8_t* s_at = smem + (S::RING > join_bytes ? S::RING : join_bytes);
+  float* s_q = reinterpret_cast<float*>(s_at);
+  s_at += R * D * 4;
+  uint4* s_frag = reinterpret_cast<uint4*>(s_at);  // [hi, lo][mb][ks][lane]
+  s_at += NARROW ? 0 : 2 * MB * KS * 512;
+  float* s_factor = reinterpret_cast<float*>(s_at);
+  int* s_limit = reinterpret_cast<int*>(s_factor + R);
+  float2* s_ml = reinterpret_cast<float2*>(s_limit + R);
+  uint32_t* s_there = reinterpret_cast<uint32_t*>(s_ml + kWarps * R);
+  int* s_last = reinterpret_cast<int*>(s_there + kWarps * kStages);
+
+  ta_wait_for_prior_grid();
+  const ta_cache_dev& c = a.cache;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3;
+  const int group = blockIdx.x / pieces, part = blockIdx.x - group * pieces;
+  const int unit = group / row_blocks, r0 = (group - unit * row_blocks) * R;
+  const Unit u = unit_of(a, unit, part == 0 && r0 == 0 && tid == 0, status);
+  const int G = a.Hq / c.Hkv, rows = G * a.T;
+  const int n_pieces = max(1, (u.n + piece - 1) / piece);  // at least one, which writes the empty result
+  if (part >= n_pieces) return;
+  const int begin = part * piece, end = min(u.n, begin + piece);
+  const int tiles = (end - begin + TK - 1) / TK, mine = tiles > warp ? (tiles - warp + kWarps - 1) / kWarps : 0;
+
+  // ---- the ring
+  const long long base = u.l * c.sl + u.g * c.sh, sbase = u.l * c.ssl + u.g * c.ssh;
+  const uint32_t ring = smem_u32(smem) + warp * kStages * S::STAGE;
+  uint32_t* there_w = s_there + warp * kStages;
+  ta_row_at at = {-1, 0};
+  auto look_up = [&](int i) {  // this lane's row of the warp's i-th tile
+    const int r = begin + (warp + i * kWarps) * TK + lane;
+    at = {-1, 0};
+    if (lane < TK && r < end) {
+      at = ta_cache_row(c, u.b, r);
+      if (at.row < 0) ta_report_bounds(status, 33, u.b, r);
     }
-    s_q[j] = v;
+  };
+  auto issue = [&](int i) {
+    if (i < mine) {
+      const int stage = i % kStages;
+      const uint32_t dst = ring + stage * S::STAGE;
+      const uint32_t there = __ballot_sync(0xffffffffu, at.row >= 0);
+      if (lane == 0) there_w[stage] = there;
+#pragma unroll
+      for (int k = 0; k < TK * S::CHUNKS / 32; ++k) {
+        const int row = (k * 32 + lane) / S::CHUNKS, ch = (k * 32 + lane) % S::CHUNKS;
+        const long long off = __shfl_sync(0xffffffffu, at.row, row);
+        const bool is = (there >> row) & 1;
+        const long long src = is ? base + off + ch * 16 : 0;
+        // swizzles: eight lanes that read 16 bytes each at a time meet all banks (keys: two rows and four chunks; values: eight
+        // rows of one chunk through ldmatrix, or, of codes, four even rows and two chunks)
+        const int kx = S::CHUNKS >= 8 ? (row & 1) << 2 : 0;
+        const int vx = !CODES ? row & 7 : S::CHUNKS >= 8 ? ((row >> 1) & 3) << 1 : (row >> 1) & 3;
+        cp16(dst + row * S::ROW + ((ch ^ kx) << 4), c.k + src, is);
+        cp16(dst + S::TILE + row * S::ROW + ((ch ^ vx) << 4), c.v + src, is);
+      }
+      if constexpr (CODES) {
+        const bool is = at.row >= 0;
+        const long long src = is ? sbase + at.scale : 0;
+        if (lane < TK) {
+          cp4(dst + 2 * S::TILE + lane * 4, c.ks + src, is);
+          cp4(dst + 2 * S::TILE + TK * 4 + lane * 4, c.vs + src, is);
+        }
+      }
+      look_up(i + 1);
+    }
+    cp_commit();
+  };
+  look_up(0);
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i) issue(i);
+
+  // ---- the queries: fp32 in shared memory, rotated, then fragments
+  for (int w = tid; w < R * D; w += kThreads) {
+    const int r = w / D, j = w - r * D, row = r0 + r;
+    float v = 0.0f;
+    if (row < rows) {
+      const int t = row / G, h = u.g * G + row - t * G;
+      const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(a.q.ptr) + u.l * a.q.stride_l + u.b * a.q.stride_b +
+                               h * a.q.stride_h + t * a.q.stride_n;
+      v = __bfloat162float(q[j]);
+      if (a.rot.phase && j < a.rot.d_rot) {
+        const int half = a.rot.d_rot / 2;
+        const int position = a.rot.positions ? a.rot.positions[u.b * a.T + t] : u.n - a.T + t;
+        const bool second = a.rot.interleaved ? (j & 1) : j >= half;
+        const int p = a.rot.interleaved ? j >> 1 : (second ? j - half : j);
+        const int other = a.rot.interleaved ? j ^ 1 : (second ? j - half : j + half);
+        const float2 cs = ta_cos_sin(a.rot, a.rot.phase[p], position);
+        const float o = __bfloat162float(q[other]);
+        v = second ? o * cs.y + v * cs.x : v * cs.x - o * cs.y;
+      }
+    }
+    s_q[w] = v;
+  }
+  if (tid < R) {
+    const int row = r0 + tid;
+    s_limit[tid] = row < rows ? max(0, u.n - (a.causal ? a.T - 1 - row / G : 0)) : 0;
   }
   __syncthreads();
-  float qf[N], o[N] = {}, m = -INFINITY, sum = 0.0f;
+  // a row's part of four coordinates for product ks: the order in which a lane's bytes of a key row come
+  auto coordinate = [&](int ks) { return CODES ? (t4 + 4 * (ks / 4)) * 16 + (ks % 4) * 4 : (t4 + 4 * (ks / 2)) * 8 + (ks % 2) * 4; };
+  const float bits = a.scale * 1.4426950408889634f;
+  auto row_scale = [&](int r, float& down) {  // 8-bit caches: a power of two that brings the row's largest value into [1, 2)
+    float m = 0.0f;
+    if constexpr (CODES) {
 #pragma unroll
-  for (int e = 0; e < N; ++e) qf[e] = s_q[lane + 32 * e];
-  float* sc = scores ? scores + ((long long)unit * gridDim.y + blockIdx.y) * a.max_len : nullptr;
-  for (int r = warp; r < seen; r += kWarps) {
-    const ta_row_at at = ta_cache_row(c, b, r);
-    if (at.row < 0) {
-      if (lane == 0) ta_report_bounds(status, 33, b, r);
-      if (sc && lane == 0) sc[r] = -INFINITY;
-      continue;
+      for (int ks = 0; ks < KS; ++ks) {
+        const float4 v = *reinterpret_cast<const float4*>(s_q + r * D + coordinate(ks));
+        m = fmaxf(m, fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w))));
+      }
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
     }
-    const long long base = l * c.sl + g * c.sh + at.row, sbase = l * c.ssl + g * c.ssh + at.scale;
-    float s = 0.0f;
+    const int e = CODES ? min(max((int)(__float_as_uint(m) >> 23) - 127, -100), 126) : 0;
+    down = pow2(-e);
+    return bits * pow2(e);
+  };
+  uint32_t qf[NARROW ? KS : 1][4];
+  float factor[NR];
+  int limit[NR];
+  if constexpr (NARROW) {
+    float down;
+    factor[0] = row_scale(g8, down);
+    limit[0] = s_limit[g8];
 #pragma unroll
-    for (int e = 0; e < N; ++e) s += qf[e] * cache_value(c, c.k + base, lane + 32 * e);
+    for (int ks = 0; ks < KS; ++ks) {
+      const float4 v = *reinterpret_cast<const float4*>(s_q + g8 * D + coordinate(ks));
+      qf[ks][0] = pack2<CODES>(v.x * down, v.y * down);
+      qf[ks][2] = pack2<CODES>(v.z * down, v.w * down);
+      qf[ks][1] = rest2<CODES>(v.x * down, v.y * down, qf[ks][0]);
+      qf[ks][3] = rest2<CODES>(v.z * down, v.w * down, qf[ks][2]);
+    }
+  } else {
+    for (int mb = warp; mb < MB; mb += kWarps) {
+      float d0, d1;
+      const float f0 = row_scale(mb * 16 + g8, d0), f1 = row_scale(mb * 16 + g8 + 8, d1);
+      if (t4 == 0) s_factor[mb * 16 + g8] = f0, s_factor[mb * 16 + g8 + 8] = f1;
 #pragma unroll
-    for (int w = 16; w > 0; w >>= 1) s += __shfl_xor_sync(0xffffffffu, s, w);
-    s *= a.scale * (c.format == TA_CACHE_BF16 ? 1.0f : c.ks[sbase]);
-    if (sc && lane == 0) sc[r] = s;
-    const float top = fmaxf(m, s), ref = top == -INFINITY ? 0.0f : top;
-    const float keep = __expf(m - ref), p = __expf(s - ref);
-    const float pv = p * (c.format == TA_CACHE_BF16 ? 1.0f : c.vs[sbase]);
-    sum = sum * keep + p;
+      for (int ks = 0; ks < KS; ++ks) {
+        const float4 v = *reinterpret_cast<const float4*>(s_q + (mb * 16 + g8) * D + coordinate(ks));
+        const float4 w = *reinterpret_cast<const float4*>(s_q + (mb * 16 + g8 + 8) * D + coordinate(ks));
+        uint4 hi, lo;
+        hi.x = pack2<CODES>(v.x * d0, v.y * d0);
+        hi.y = pack2<CODES>(w.x * d1, w.y * d1);
+        hi.z = pack2<CODES>(v.z * d0, v.w * d0);
+        hi.w = pack2<CODES>(w.z * d1, w.w * d1);
+        lo.x = rest2<CODES>(v.x * d0, v.y * d0, hi.x);
+        lo.y = rest2<CODES>(w.x * d1, w.y * d1, hi.y);
+        lo.z = rest2<CODES>(v.z * d0, v.w * d0, hi.z);
+        lo.w = rest2<CODES>(w.z * d1, w.w * d1, hi.w);
+        s_frag[(mb * KS + ks) * 32 + lane] = hi;
+        s_frag[((MB + mb) * KS + ks) * 32 + lane] = lo;
+      }
+    }
+    __syncthreads();
 #pragma unroll
-    for (int e = 0; e < N; ++e) o[e] = o[e] * keep + pv * cache_value(c, c.v + base, lane + 32 * e);
-    m = top;
+    for (int i = 0; i < NR; ++i) {
+      factor[i] = s_factor[(i / 2) * 16 + (i & 1) * 8 + g8];
+      limit[i] = s_limit[(i / 2) * 16 + (i & 1) * 8 + g8];
+    }
   }
-  if (lane == 0) s_m[warp] = m, s_l[warp] = sum;
+  const bool q_parts = a.rot.phase != nullptr;  // queries that are not rotated have no second part
+  const uint32_t frag = smem_u32(s_frag) + lane * 16;
+  const int seen_by_all = s_limit[0];  // the block's first row has the lowest limit
+
+  float o[MBN][NJ][4], m[NR], l[NR];
 #pragma unroll
-  for (int e = 0; e < N; ++e) s_o[warp][lane + 32 * e] = o[e];
+  for (int i = 0; i < NR; ++i) m[i] = -INFINITY, l[i] = 0.0f;
+#pragma unroll
+  for (int i = 0; i < MBN; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[i][j][e] = 0.0f;
+  int ref = -100;  // 8-bit caches: exponent that the value rows' scales are taken relative to
+
+  for (int i = 0; i < mine; ++i) {
+    cp_wait<kStages - 2>();
+    __syncwarp();
+    issue(i + kStages - 1);
+    const int stage = i % kStages, first = begin + (warp + i * kWarps) * TK;
+    const uint32_t kt = ring + stage * S::STAGE, vt = kt + S::TILE, st = kt + 2 * S::TILE;
+    const uint32_t there = there_w[stage];
+    const bool whole = there == (TK == 32 ? 0xffffffffu : (1u << TK) - 1) && first + TK <= seen_by_all;
+
+    // ---- scores
+    float s[MBN][NT][4];
+#pragma unroll
+    for (int x = 0; x < MBN; ++x)
+#pragma unroll
+      for (int y = 0; y < NT; ++y)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[x][y][e] = 0.0f;
+    constexpr int PER = CODES ? 4 : 2;  // products that 16 bytes of a key row serve
+#pragma unroll
+    for (int k = 0; k < KS / PER; ++k) {
+      uint4 w[NT];
+#pragma unroll
+      for (int y = 0; y < NT; ++y) {
+        const int kx = S::CHUNKS >= 8 ? (g8 & 1) << 2 : 0;
+        w[y] = lds128(kt + (y * 8 + g8) * S::ROW + (((t4 + 4 * k) ^ kx) << 4));
+      }
+#pragma unroll
+      for (int h = 0; h < PER; ++h) {
+        uint32_t b0[NT], b1[NT];
+#pragma unroll
+        for (int y = 0; y < NT; ++y) {
+          const uint32_t* wy = reinterpret_cast<const uint32_t*>(&w[y]);
+          if constexpr (CODES) expand<FMT>(wy[h], b0[y], b1[y]);
+          else b0[y] = wy[2 * h], b1[y] = wy[2 * h + 1];
+        }
+        if constexpr (NARROW) {
+#pragma unroll
+          for (int y = 0; y < NT; ++y) mma<CODES>(s[0][y], qf[k * PER + h], b0[y], b1[y]);
+        } else {
+#pragma unroll
+          for (int x = 0; x < MB; ++x) {
+            uint4 q = lds128(frag + (x * KS + k * PER + h) * 512);
+            const uint32_t qa[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int y = 0; y < NT; ++y) mma<CODES>(s[x][y], qa, b0[y], b1[y]);
+            if (q_parts) {
+              q = lds128(frag + ((MB + x) * KS + k * PER + h) * 512);
+              const uint32_t ql[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+              for (int y = 0; y < NT; ++y) mma<CODES>(s[x][y], ql, b0[y], b1[y]);
+            }
+          }
+        }
+      }
+    }
+    // this thread's scores, in bits: x[row][8-row tile][2]
+    float x[NR][NT][2];
+    float2 vs[NT];
+#pragma unroll
+    for (int y = 0; y < NT; ++y) {
+      float2 ks = make_float2(1.0f, 1.0f);
+      vs[y] = ks;
+      if constexpr (CODES) {
+        ks = lds_f2(st + (y * 8 + 2 * t4) * 4);
+        vs[y] = lds_f2(st + (TK + y * 8 + 2 * t4) * 4);
+      }
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {
+        if constexpr (NARROW) {
+          x[0][y][0] = (s[0][y][0] + s[0][y][2]) * (factor[0] * ks.x);
+          x[0][y][1] = (s[0][y][1] + s[0][y][3]) * (factor[0] * ks.y);
+        } else {
+          x[r][y][0] = s[r / 2][y][(r & 1) * 2] * (factor[r] * ks.x);
+          x[r][y][1] = s[r / 2][y][(r & 1) * 2 + 1] * (factor[r] * ks.y);
+        }
+      }
+    }
+    if (!whole) {
+#pragma unroll
+      for (int y = 0; y < NT; ++y)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int k = y * 8 + 2 * t4 + e;
+          const bool is = (there >> k) & 1;
+#pragma unroll
+          for (int r = 0; r < NR; ++r)
+            if (!is || first + k >= limit[r]) x[r][y][e] = -INFINITY;
+        }
+    }
+    if (sc.score) {
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {
+        const int row = r0 + (NARROW ? g8 : (r / 2) * 16 + (r & 1) * 8 + g8);
+        if (row < rows) {
+          float* to = sc.score + ((long long)unit * rows + row) * sc.score_stride + first;
+#pragma unroll
+          for (int y = 0; y < NT; ++y)
+            if (first + y * 8 + 2 * t4 < end) *reinterpret_cast<float2*>(to + y * 8 + 2 * t4) = make_float2(x[r][y][0], x[r][y][1]);
+        }
+      }
+    }
+
+    // ---- running maximum and sum
+    float keep[NR];
+    bool grew = false;
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+      float top = m[r];
+#pragma unroll
+      for (int y = 0; y < NT; ++y) top = fmaxf(top, fmaxf(x[r][y][0], x[r][y][1]));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const float from = top == -INFINITY ? 0.0f : top;
+      keep[r] = ex2(m[r] - from);
+      grew |= top > m[r];
+      m[r] = top;
+      float sum = 0.0f;
+#pragma unroll
+      for (int y = 0; y < NT; ++y) {
+        x[r][y][0] = ex2(x[r][y][0] - from);
+        x[r][y][1] = ex2(x[r][y][1] - from);
+        sum += x[r][y][0] + x[r][y][1];
+      }
+      l[r] = l[r] * keep[r] + sum;
+    }
+    if constexpr (CODES) {
+      // probabilities times their value rows' scales, relative to 2^ref and times 2^14: at most 2^15, and 2^-38 of the largest
+      // is still told from zero. Scales that are not finite set no reference.
+      uint32_t top = lane < TK ? lds32(st + (TK + lane) * 4) & 0x7fffffffu : 0;
+      top = __reduce_max_sync(0xffffffffu, top >= 0x7f800000u ? 0 : top);
+      const int e = (int)(top >> 23) - 127;
+      if (e > ref) {
+        const float down = ref - e < -126 ? 0.0f : pow2(ref - e);
+#pragma unroll
+        for (int r = 0; r < NR; ++r) keep[r] *= down;
+        ref = e;
+        grew = true;
+      }
+      const float up = pow2(min(14 - ref, 127));
+#pragma unroll
+      for (int y = 0; y < NT; ++y) {
+        vs[y].x *= up;
+        vs[y].y *= up;
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+          x[r][y][0] = !whole && x[r][y][0] == 0.0f ? 0.0f : x[r][y][0] * vs[y].x;  // (a scale that is not seen may be NaN)
+          x[r][y][1] = !whole && x[r][y][1] == 0.0f ? 0.0f : x[r][y][1] * vs[y].y;
+        }
+      }
+    }
+    if (__any_sync(0xffffffffu, grew)) {
+#pragma unroll
+      for (int y = 0; y < MBN; ++y)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          const float k0 = keep[NARROW ? 0 : 2 * y], k1 = keep[NARROW ? 0 : 2 * y + 1];
+          o[y][j][0] *= k0;
+          o[y][j][1] *= k0;
+          o[y][j][2] *= k1;
+          o[y][j][3] *= k1;
+        }
+    }
+
+    // ---- values. Rows that a later token sees and an earlier one does not meet probabilities of zero; where such a row is
+    // not finite, every token's rows are taken by themselves.
+    bool apart = false;
+    if (first + TK > seen_by_all && seen_by_all < end) {
+      bool bad = false;
+      for (int w = lane; w < TK * S::CHUNKS; w += 32) {
+        const int row = w / S::CHUNKS;
+        if (first + row < seen_by_all) continue;
+        const uint4 v = lds128(vt + row * S::ROW + (w % S::CHUNKS) * 16);
+        const uint32_t* p = reinterpret_cast<const uint32_t*>(&v);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if constexpr (FMT == TA_CACHE_BF16) bad |= (p[k] & 0x7f80u) == 0x7f80u || (p[k] & 0x7f800000u) == 0x7f800000u;
+          else if constexpr (FMT == TA_CACHE_E4M3)
+            bad |= (p[k] & 0x7fu) == 0x7fu || (p[k] & 0x7f00u) == 0x7f00u || (p[k] & 0x7f0000u) == 0x7f0000u ||
+                   (p[k] & 0x7f000000u) == 0x7f000000u;
+        }
+      }
+      apart = __any_sync(0xffffffffu, bad);
+    }
+#pragma unroll
+    for (int kk = 0; kk < TK / 16; ++kk) {
+      uint32_t ph[MBN][4], pl[MBN][4];
+#pragma unroll
+      for (int y = 0; y < MBN; ++y) {
+        if constexpr (NARROW) {
+          ph[0][0] = pack2<CODES>(x[0][2 * kk][0], x[0][2 * kk][1]);
+          ph[0][2] = pack2<CODES>(x[0][2 * kk + 1][0], x[0][2 * kk + 1][1]);
+          ph[0][1] = rest2<CODES>(x[0][2 * kk][0], x[0][2 * kk][1], ph[0][0]);
+          ph[0][3] = rest2<CODES>(x[0][2 * kk + 1][0], x[0][2 * kk + 1][1], ph[0][2]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = 2 * y + (e & 1), tile = 2 * kk + (e >> 1);
+            ph[y][e] = pack2<CODES>(x[r][tile][0], x[r][tile][1]);
+            pl[y][e] = rest2<CODES>(x[r][tile][0], x[r][tile][1], ph[y][e]);
+          }
+        }
+      }
+      auto product = [&](int j, uint32_t b0, uint32_t b1) {
+        if (!apart) {
+#pragma unroll
+          for (int y = 0; y < MBN; ++y) {
+            mma<CODES>(o[y][j], ph[y], b0, b1);
+            if constexpr (!NARROW) mma<CODES>(o[y][j], pl[y], b0, b1);
+          }
+          return;
+        }
+        int before = -1;
+        for (int r = 0; r < R; ++r) {  // one product per limit; a row takes the result of its own
+          const int lim = s_limit[r];
+          if (lim == before) continue;
+          before = lim;
+          auto cut = [&](uint32_t v, int k) {
+            if (first + kk * 16 + k >= lim) v &= 0xffff0000u;
+            if (first + kk * 16 + k + 1 >= lim) v &= 0x0000ffffu;
+            return v;
+          };
+          const uint32_t c0 = cut(b0, 2 * t4), c1 = cut(b1, 2 * t4 + 8);
+#pragma unroll
+          for (int y = 0; y < MBN; ++y) {
+            float own[4] = {o[y][j][0], o[y][j][1], o[y][j][2], o[y][j][3]};
+            mma<CODES>(own, ph[y], c0, c1);
+            if constexpr (!NARROW) mma<CODES>(own, pl[y], c0, c1);
+            const bool u0 = limit[NARROW ? 0 : 2 * y] == lim, u1 = limit[NARROW ? 0 : 2 * y + 1] == lim;
+            if (u0) o[y][j][0] = own[0], o[y][j][1] = own[1];
+            if (u1) o[y][j][2] = own[2], o[y][j][3] = own[3];
+          }
+        }
+      };
+      if constexpr (!CODES) {
+#pragma unroll
+        for (int j = 0; j < NJ / 2; ++j) {
+          const int key = kk * 16 + ((lane >> 3) & 1) * 8 + (lane & 7), ch = 2 * j + (lane >> 4);
+          uint32_t b[4];
+          ldmatrix4_trans(b, vt + key * S::ROW + ((ch ^ (key & 7)) << 4));
+          product(2 * j, b[0], b[1]);
+          product(2 * j + 1, b[2], b[3]);
+        }
+      } else {
+        constexpr int W = D / 32;  // words of a lane's part of a row: D / 8 coordinates
+        uint32_t v[4][W];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int key = kk * 16 + 2 * t4 + (e & 1) + (e >> 1) * 8;
+          if constexpr (W == 4) {
+            const uint4 q = lds128(vt + key * S::ROW + ((g8 ^ (((key >> 1) & 3) << 1)) << 4));
+            v[e][0] = q.x, v[e][1] = q.y, v[e][2] = q.z, v[e][3] = q.w;
+          } else {
+            const uint2 q = lds64(vt + key * S::ROW + (((g8 >> 1) ^ ((key >> 1) & 3)) << 4) + (g8 & 1) * 8);
+            v[e][0] = q.x, v[e][1] = q.y;
+          }
+        }
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+          uint32_t b0[4], b1[4];  // pairs of two rows, one coordinate each
+          expand<FMT>(__byte_perm(v[0][w], v[1][w], 0x5140), b0[0], b0[1]);
+          expand<FMT>(__byte_perm(v[0][w], v[1][w], 0x7362), b0[2], b0[3]);
+          expand<FMT>(__byte_perm(v[2][w], v[3][w], 0x5140), b1[0], b1[1]);
+          expand<FMT>(__byte_perm(v[2][w], v[3][w], 0x7362), b1[2], b1[3]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) product(4 * w + e, b0[e], b1[e]);
+        }
+      }
+    }
+  }
+
+  // ---- the warps join
+  cp_wait<0>();
+  __syncthreads();  // the rings are free
+  constexpr int LD = D + 4;
+  float* s_o = reinterpret_cast<float*>(smem);
+  const float unit_of_o = CODES ? pow2(max(ref - 14, -126)) : 1.0f;
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+    l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+    const int row = NARROW ? g8 : (r / 2) * 16 + (r & 1) * 8 + g8;
+    if (t4 == 0) s_ml[warp * R + row] = make_float2(m[r], l[r]);
+    float* to = s_o + (warp * R + row) * LD;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const float v0 = NARROW ? o[0][j][0] + o[0][j][2] : o[r / 2][j][(r & 1) * 2];
+      const float v1 = NARROW ? o[0][j][1] + o[0][j][3] : o[r / 2][j][(r & 1) * 2 + 1];
+      if constexpr (CODES) {
+        to[2 * t4 * NJ + j] = v0 * unit_of_o;
+        to[(2 * t4 + 1) * NJ + j] = v1 * unit_of_o;
+      } else {
+        *reinterpret_cast<float2*>(to + j * 8 + 2 * t4) = make_float2(v0, v1);
+      }
+    }
+  }
   __syncthreads();
-  float top = -INFINITY, z = 0.0f;
-  for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_m[w]);
-  const float ref = top == -INFINITY ? 0.0f : top;
-  for (int w = 0; w < kWarps; ++w) z += s_l[w] == 0.0f ? 0.0f : s_l[w] * __expf(s_m[w] - ref);
-  __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(const_cast<void*>(a.out.ptr)) + l * a.out.stride_l + b * a.out.stride_b +
-                       h * a.out.stride_h + t * a.out.stride_n;
-  for (int j = threadIdx.x; j < D; j += kWarps * 32) {
-    float x = 0.0f;
-    for (int w = 0; w < kWarps; ++w) x += s_l[w] == 0.0f ? 0.0f : s_o[w][j] * __expf(s_m[w] - ref);
-    out[j] = __float2bfloat16(z == 0.0f ? 0.0f : x / z);
+  auto finish = [&](int row, int j, float mm, float ll, float4 x) {
+    const int t = row / G, h = u.g * G + row - t * G;
+    const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;  // (a sum of NaN stays one)
+    __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(const_cast<void*>(a.out.ptr)) + u.l * a.out.stride_l +
+                         u.b * a.out.stride_b + h * a.out.stride_h + t * a.out.stride_n;
+    *reinterpret_cast<uint2*>(out + j) = make_uint2(pack2<false>(x.x * inv, x.y * inv), pack2<false>(x.z * inv, x.w * inv));
+    if (j == 0) {
+      if (a.lse)
+        a.lse[(((long long)u.l * c.batch + u.b) * a.Hq + h) * a.T + t] =
+            ll == 0.0f ? -INFINITY : mm * 0.6931471805599453f + logf(ll);
+      if (sc.row_ml) sc.row_ml[(long long)unit * rows + row] = make_float2(mm, inv);
+    }
+  };
+  const int n_rows = min(R, rows - r0);
+  for (int w = tid; w < n_rows * (D / 4); w += kThreads) {
+    const int r = w / (D / 4), j = (w - r * (D / 4)) * 4;
+    float mm = -INFINITY, ll = 0.0f;
+    float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int k = 0; k < kWarps; ++k) mm = fmaxf(mm, s_ml[k * R + r].x);
+    const float from = mm == -INFINITY ? 0.0f : mm;
+#pragma unroll
+    for (int k = 0; k < kWarps; ++k) {
+      const float2 ml = s_ml[k * R + r];
+      const float f = ex2(ml.x - from);
+      const float4 y = *reinterpret_cast<const float4*>(s_o + (k * R + r) * LD + j);
+      if (ml.y == 0.0f) continue;
+      ll += ml.y * f;
+      x.x += y.x * f;
+      x.y += y.y * f;
+      x.z += y.z * f;
+      x.w += y.w * f;
+    }
+    if (n_pieces == 1) {
+      finish(r0 + r, j, mm, ll, x);
+    } else {
+      const long long slot = ((long long)group * pieces + part) * R + r;
+      *reinterpret_cast<float4*>(sc.part + slot * D + j) = x;
+      if (j == 0) sc.part_ml[slot] = make_float2(mm, ll);
+    }
   }
-  if (threadIdx.x == 0) {
-    const float lse = z == 0.0f ? -INFINITY : ref + logf(z);
-    if (a.lse) a.lse[(((long long)l * c.batch + b) * a.Hq + h) * a.T + t] = lse;
-    if (row_lse) row_lse[(long long)unit * gridDim.y + blockIdx.y] = lse;
+  if (n_pieces == 1) return;
+
+  // ---- the pieces join: the block that comes last reads them in their order
+  __threadfence();
+  __syncthreads();
+  if (tid == 0) {
+    const int came = atomicAdd(&sc.ticket[group], 1);
+    *s_last = came == n_pieces - 1;
+    if (*s_last) sc.ticket[group] = 0;
+  }
+  __syncthreads();
+  if (!*s_last) return;
+  __threadfence();
+  for (int w = tid; w < n_rows * (D / 4); w += kThreads) {
+    const int r = w / (D / 4), j = (w - r * (D / 4)) * 4;
+    const long long slot = (long long)group * pieces * R + r;
+    const float mm = joined_max(sc.part_ml + slot, n_pieces, R), from = mm == -INFINITY ? 0.0f : mm;
+    float ll = 0.0f;
+    float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+    for (int k = 0; k < n_pieces; ++k) {
+      const float2 ml = __ldcg(&sc.part_ml[slot + (long long)k * R]);
+      const float4 y = __ldcg(reinterpret_cast<const float4*>(sc.part + (slot + (long long)k * R) * D + j));
+      const float f = ml.y == 0.0f ? 0.0f : ex2(ml.x - from);
+      if (ml.y == 0.0f) continue;
+      ll += ml.y * f;
+      x.x += y.x * f;
+      x.y += y.y * f;
+      x.z += y.z * f;
+      x.w += y.w * f;
+    }
+    finish(r0 + r, j, mm, ll, x);
   }
 }
 
-// Attention mass per cache row. grid.x = units, grid.y = blocks of rows.
-__global__ void __launch_bounds__(256) ta_attend_mass_kernel(ta_attend_args a, const float* scores, const float* row_lse) {
+// Attention mass per cache row, from the scores and the rows' maxima and sums. grid.x = units, grid.y = stretches of rows.
+__global__ void __launch_bounds__(256) ta_attend_mass_kernel(ta_attend_args a, Scratch sc) {
   ta_wait_for_prior_grid();
-  const ta_cache_dev& c = a.cache;
-  const int unit = blockIdx.x, g = unit % c.Hkv, b = unit / c.Hkv % c.batch, l = unit / c.Hkv / c.batch;
-  const int G = a.Hq / c.Hkv, R = G * a.T;
-  long long n = (long long)ta_cache_len(c, l, b, g) + a.new_rows;
-  n = min(n, min((long long)a.max_len, (long long)c.wide * c.page));
-  for (long long j = blockIdx.y * 256 + threadIdx.x; j < a.mass_stride; j += gridDim.y * 256) {
-    float m = 0.0f;
-    for (int r = 0; r < R; ++r) {
-      const long long seen = n - (a.causal ? a.T - 1 - r / G : 0);
-      if (j < seen) m += __expf(scores[((long long)unit * R + r) * a.max_len + j] - row_lse[(long long)unit * R + r]);
+  const int unit = blockIdx.x;
+  const Unit u = unit_of(a, unit, false, nullptr);
+  const int G = a.Hq / a.cache.Hkv, rows = G * a.T;
+  for (long long j = (long long)blockIdx.y * 256 + threadIdx.x; j < a.mass_stride; j += (long long)gridDim.y * 256) {
+    float sum = 0.0f;
+    for (int r = 0; r < rows; ++r) {
+      if (j >= u.n - (a.causal ? a.T - 1 - r / G : 0)) continue;
+      const float2 ml = sc.row_ml[(long long)unit * rows + r];
+      if (ml.y == 0.0f) continue;  // a token that sees nothing
+      sum += ex2(sc.score[((long long)unit * rows + r) * sc.score_stride + j] - ml.x) * ml.y;
     }
-    a.mass[unit * a.mass_stride + j] = m;
+    a.mass[unit * a.mass_stride + j] = sum;
   }
+}
+
+// How a call is cut: query rows of a block, and pieces of the cache rows. Sized for the 148 SMs of a B200 at two blocks each.
+struct Plan {
+  int mb, row_blocks, piece, pieces;
+};
+constexpr int kSlots = 2 * 148;
+constexpr int kPieceUnit = 128;  // rows: whole rounds of every variant's four warps
+Plan plan_of(long long units, int rows, int max_len) {
+  Plan p;
+  p.mb = rows <= 8 ? 0 : rows <= 16 ? 1 : 2;
+  p.row_blocks = (rows + rows_of(p.mb) - 1) / rows_of(p.mb);
+  const long long groups = units * p.row_blocks;
+  long long want = groups > kAttendTickets ? 1 : (kSlots + groups - 1) / groups;
+  p.piece = (int)(((max_len + want - 1) / want + kPieceUnit - 1) / kPieceUnit * kPieceUnit);
+  if (p.piece < kPieceUnit) p.piece = kPieceUnit;
+  p.pieces = (max_len + p.piece - 1) / p.piece;
+  if (p.pieces < 1) p.pieces = 1;
+  return p;
+}
+constexpr size_t up(size_t x) { return (x + 255) / 256 * 256; }
+
+template <int D, int FMT, int MB>
+cudaError_t launch(const ta_attend_args& a, const Scratch& sc, const Plan& p, cudaLaunchConfig_t& cfg, ta_dev_status* status) {
+  constexpr int smem = smem_bytes<D, FMT, MB>();
+  static bool set[64] = {};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (!set[dev & 63]) {
+    e = cudaFuncSetAttribute(ta_attend_kernel<D, FMT, MB>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    set[dev & 63] = true;
+  }
+  cfg.dynamicSmemBytes = smem;
+  return cudaLaunchKernelEx(&cfg, ta_attend_kernel<D, FMT, MB>, a, sc, p.pieces, p.piece, p.row_blocks, status);
+}
+template <int D, int FMT>
+cudaError_t launch(const ta_attend_args& a, const Scratch& sc, const Plan& p, cudaLaunchConfig_t& cfg, ta_dev_status* status) {
+  if (p.mb == 0) return launch<D, FMT, 0>(a, sc, p, cfg, status);
+  if (p.mb == 1) return launch<D, FMT, 1>(a, sc, p, cfg, status);
+  return launch<D, FMT, 2>(a, sc, p, cfg, status);
+}
+template <int D>
+cudaError_t launch(const ta_attend_args& a, const Scratch& sc, const Plan& p, cudaLaunchConfig_t& cfg, ta_dev_status* status) {
+  if (a.cache.format == TA_CACHE_BF16) return launch<D, TA_CACHE_BF16>(a, sc, p, cfg, status);
+  if (a.cache.format == TA_CACHE_E4M3) return launch<D, TA_CACHE_E4M3>(a, sc, p, cfg, status);
+  return launch<D, TA_CACHE_INT8>(a, sc, p, cfg, status);
+}
+
+size_t carve(long long units, int rows, int d, int max_len, bool with_mass, uint8_t* base, Scratch* sc) {
+  const Plan p = plan_of(units, rows, max_len);
+  const size_t slots = p.pieces > 1 ? (size_t)units * p.row_blocks * p.pieces * rows_of(p.mb) : 0;
+  const long long stride = (max_len + 31) / 32 * 32;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    uint8_t* at = base + off;
+    off += up(bytes);
+    return at;
+  };
+  Scratch s = {};
+  s.part = reinterpret_cast<float*>(take(slots * d * 4));
+  s.part_ml = reinterpret_cast<float2*>(take(slots * 8));
+  if (with_mass) {
+    s.score_stride = stride;
+    s.score = reinterpret_cast<float*>(take((size_t)units * rows * stride * 4));
+    s.row_ml = reinterpret_cast<float2*>(take((size_t)units * rows * 8));
+  }
+  if (sc) *sc = s;
+  return off;
 }
 
 }  // namespace
 
 size_t ta_attend_scratch(int units, int rows, int d, int max_len, bool with_mass) {
-  return with_mass ? (size_t)units * rows * ((size_t)max_len + 1) * 4 : 0;
+  return carve(units, rows, d, max_len, with_mass, nullptr, nullptr);
 }
 
-cudaError_t ta_launch_attend(const ta_attend_args& a, ta_dev_status* status, cudaStream_t stream) {
+cudaError_t ta_launch_attend(const ta_attend_args& a, int* tickets, ta_dev_status* status, cudaStream_t stream) {
   const int units = a.n_layers * a.cache.batch * a.cache.Hkv, rows = a.Hq / a.cache.Hkv * a.T;
-  float* row_lse = a.mass ? reinterpret_cast<float*>(a.scratch) : nullptr;
-  float* scores = a.mass ? row_lse + (size_t)units * rows : nullptr;
+  const Plan p = plan_of(units, rows, a.max_len);
+  Scratch sc;
+  carve(units, rows, a.d, a.max_len, a.mass != nullptr, a.scratch, &sc);
+  sc.ticket = tickets;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)units, (unsigned)rows, 1);
-  cfg.blockDim = dim3(kWarps * 32, 1, 1);
+  cfg.gridDim = dim3((unsigned)((long long)units * p.row_blocks * p.pieces), 1, 1);
+  cfg.blockDim = dim3(kThreads, 1, 1);
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   ta_pdl_attribute(&attr[0]);
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  cudaError_t e = a.d == 64 ? cudaLaunchKernelEx(&cfg, ta_attend_kernel<64>, a, scores, row_lse, status)
-                            : cudaLaunchKernelEx(&cfg, ta_attend_kernel<128>, a, scores, row_lse, status);
+  cudaError_t e = a.d == 64 ? launch<64>(a, sc, p, cfg, status) : launch<128>(a, sc, p, cfg, status);
   if (e != cudaSuccess || !a.mass) return e;
   cfg.gridDim = dim3((unsigned)units, (unsigned)((a.mass_stride + 255) / 256), 1);
   cfg.blockDim = dim3(256, 1, 1);
-  return cudaLaunchKernelEx(&cfg, ta_attend_mass_kernel, a, (const float*)scores, (const float*)row_lse);
+  cfg.dynamicSmemBytes = 0;
+  return cudaLaunchKernelEx(&cfg, ta_attend_mass_kernel, a, sc);
 }

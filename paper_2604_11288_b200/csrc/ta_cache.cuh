@@ -59,7 +59,8 @@ struct ta_attend_args {
   uint8_t* scratch;
 };
 size_t ta_attend_scratch(int units, int rows, int d, int max_len, bool with_mass);
-cudaError_t ta_launch_attend(const ta_attend_args& a, ta_dev_status* status, cudaStream_t stream);
+// tickets: kAttendTickets words, zero before and after
+cudaError_t ta_launch_attend(const ta_attend_args& a, int* tickets, ta_dev_status* status, cudaStream_t stream);
 
 #ifdef __CUDACC__
 // Cosine and sine of a position's angle, with the factor on both: the product modulo 2^64 is the angle in turns, exactly, and

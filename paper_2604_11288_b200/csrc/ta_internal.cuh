@@ -45,6 +45,8 @@ struct ta_stream_sync {
   unsigned long long hold_ns;  // 0; in the self-test: how long the first blocks hold their words back
 };
 
+constexpr int kAttendTickets = 16384;  // units and row blocks of an attention call whose cache rows are cut into pieces
+
 struct ta_ctx {
   int device;
   int sm_count;
@@ -53,6 +55,7 @@ struct ta_ctx {
   uint8_t* scratch;         // device
   ta_dev_status* d_status;  // device
   ta_stream_sync stream_sync;  // of the decode step
+  int* attend_tickets;         // device [kAttendTickets], 0 between launches
   // cache of per-sequence results inside scratch (ta_compress)
   uint64_t cached_epoch;
   uint64_t cached_key;  // policy fields and pattern set the cached results were computed with
