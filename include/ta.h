@@ -521,7 +521,8 @@ ta_status ta_rotate(ta_ctx* ctx, const ta_batch* batch, int Hq, int Hkv, int d, 
  *   k + l*stride_l + page_id*stride_p + g*stride_h + (r % page)*stride_r   (elements; v likewise, scales with their own)
  * table NULL: the sequence's pages are b * pages_per_seq + r / page (with page rows a sequence: one dense row block each).
  * Strides in elements, multiples of 16 bytes (scale strides: any), not negative; k and v 16-byte aligned; d 64 or 128. What
- * a table holds behind the pages that a call reaches is not read. */
+ * a table holds behind the pages that a call reaches is not read. The pages of one layer and head span less than 64 GiB and
+ * 2^32 scales, layers and heads as much as they like. */
 enum { TA_CACHE_BF16 = 0, TA_CACHE_E4M3 = 1, TA_CACHE_INT8 = 2 };
 typedef struct ta_cache {
   void *k, *v;               /* DEVICE */
@@ -571,7 +572,8 @@ ta_status ta_cache_read(ta_ctx* ctx, const ta_cache* cache, const ta_batch* batc
  * outside 0..n_pages-1 are left out; both are reported (TA_ERR_DEVICE_BOUNDS). T <= TA_MAX_NEW_TOKENS, Hq / Hkv <= 256,
  * max_len <= TA_MAX_SEQ_LEN. Products are of bf16 values (8-bit codes are exact in them; probabilities and rotated queries
  * keep 16 bits), sums and softmax statistics are in 32 bits. Scratch: ta_attend_scratch_bytes (not kept between calls; what
- * ta_compress keeps under a seq_epoch is dropped). */
+ * ta_compress keeps under a seq_epoch is dropped). The two codes of E4M3 that mean NaN, which ta_cache_append does not
+ * write, count as 480 here. */
 enum { TA_MAX_NEW_TOKENS = 64 };
 ta_status ta_attend_scratch_bytes(const ta_cache* cache, int Hq, int T, int max_len, int with_mass, size_t* out_bytes);
 ta_status ta_attend(ta_ctx* ctx, const ta_cache* cache, int Hq, int T, int new_rows, int max_len, int causal, float scale,

@@ -1088,6 +1088,10 @@ ta_status check_cache(const ta_cache* c) {
   if (codes && (c->scale_stride_l < 0 || c->scale_stride_p < 0 || c->scale_stride_h < 0 || c->scale_stride_r < 0))
     return TA_ERR_INVALID_ARG;
   if (!c->lens && c->len_uniform < 0) return TA_ERR_INVALID_ARG;
+  // a row's place within its layer and head is kept in 32 bits: in units of 16 bytes, and of a scale
+  const double far = (double)(c->n_pages - 1) * c->stride_p + (double)(c->page - 1) * c->stride_r;
+  const double far_scale = (double)(c->n_pages - 1) * c->scale_stride_p + (double)(c->page - 1) * c->scale_stride_r;
+  if (far * (codes ? 1 : 2) >= 0x1p36 || (codes && far_scale >= 0x1p32)) return TA_ERR_UNSUPPORTED;
   return TA_OK;
 }
 ta_cache_dev cache_dev(const ta_cache& c) {
@@ -1254,7 +1258,7 @@ ta_status ta_attend_scratch_bytes(const ta_cache* cache, int Hq, int T, int max_
   ta_status s = check_attend(cache, Hq, T, max_len);
   if (s != TA_OK) return s;
   *out_bytes = align_up(ta_attend_scratch(cache->n_layers * cache->batch * cache->Hkv, Hq / cache->Hkv * T, cache->d, max_len,
-                                          with_mass != 0)) +
+                                          cache->format != TA_CACHE_BF16, with_mass != 0)) +
                kAlign;
   return TA_OK;
 }
@@ -1271,7 +1275,8 @@ ta_status ta_attend(ta_ctx* ctx, const ta_cache* cache, int Hq, int T, int new_r
   if (s != TA_OK) return s;
   if (new_rows < 0 || !(scale >= 0.0f) || !isfinite(scale) || (mass && mass_stride < max_len)) return TA_ERR_INVALID_ARG;
   const int units = cache->n_layers * cache->batch * cache->Hkv;
-  if (ta_attend_scratch(units, Hq / cache->Hkv * T, cache->d, max_len, mass != nullptr) > ctx->scratch_bytes)
+  if (ta_attend_scratch(units, Hq / cache->Hkv * T, cache->d, max_len, cache->format != TA_CACHE_BF16, mass != nullptr) >
+      ctx->scratch_bytes)
     return TA_ERR_SCRATCH_TOO_SMALL;
   DeviceGuard guard(ctx->device);
   ctx->cached_epoch = 0;

@@ -31,7 +31,6 @@ using ta_sm100::smem_u32;
 
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
-constexpr int kStages = 3;
 
 template <int D, int FMT>
 struct Shape {
@@ -41,18 +40,18 @@ struct Shape {
   static constexpr int TK = (CODES || D == 64) ? 32 : 16;         // cache rows of a tile
   static constexpr int TILE = TK * ROW;                           // bytes of K, and of V, in a stage
   static constexpr int STAGE = 2 * TILE + (CODES ? 2 * TK * 4 : 0);
+  static constexpr int STAGES = CODES ? 2 : 3;
   static constexpr int KS = D / 16;                               // products along d
-  static constexpr int RING = kWarps * kStages * STAGE;
+  static constexpr int RING = kWarps * STAGES * STAGE;
 };
 __host__ __device__ constexpr int rows_of(int MB) { return MB == 0 ? 8 : 16 * MB; }  // query rows of a block
 template <int D, int FMT, int MB>
 constexpr int smem_bytes() {
   constexpr int R = rows_of(MB);
-  constexpr int q32 = R * D * 4;                             // queries in fp32
-  constexpr int frag = MB == 0 ? 0 : 2 * MB * (D / 16) * 512;  // their fragments, hi and lo
+  constexpr int q32 = R * D * 4;  // queries in fp32, then (MB > 0) their fragments, hi and lo, in the same place
   constexpr int join = kWarps * R * (D + 4) * 4;
   constexpr int ring = Shape<D, FMT>::RING > join ? Shape<D, FMT>::RING : join;
-  return ring + q32 + frag + R * 8 /* row factor, limit */ + kWarps * R * 8 /* m, l */ + kWarps * kStages * 4 + 16;
+  return ring + q32 + R * 8 /* row factor, limit */ + kWarps * R * 8 /* m, l */ + kWarps * Shape<D, FMT>::STAGES * 4 + 16;
 }
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool there) {
@@ -119,18 +118,43 @@ __device__ __forceinline__ uint32_t rest2(float x, float y, uint32_t hi) {
   const float2 h = unpack2<CODES>(hi);
   return pack2<CODES>(x - h.x, y - h.y);
 }
-// four codes as two pairs of fp16, exactly
-template <int FMT>
-__device__ __forceinline__ void expand(uint32_t w, uint32_t& lo, uint32_t& hi) {
+// Codes as fp16, exactly, without the conversion unit (16 lanes a clock: cvt.f16x2.e4m3x2 kept the whole kernel at a fifth of the
+// memory's rate). Bytes i of x and y become a pair:
+//   E4M3: both bytes with their signs spread over the byte above (one permute), shifted so that the four exponent and three
+//     mantissa bits stand where fp16 has the last four and first three of its own, the sign that lands on the fifth exponent
+//     bit masked out: the value times 2^-8 (kCodeUnit), subnormals included. The shift is a product with a number that the
+//     compiler does not know: the other two instructions load the integer pipe, this one the multipliers.
+//   INT8: the byte with its upper bit turned over is c + 128; under the exponent of 1024 that is 1152 + c, less 1152.
+template <int FMT, int I>
+__device__ __forceinline__ uint32_t pair_of(uint32_t x, uint32_t y, uint32_t times128) {
   if constexpr (FMT == TA_CACHE_E4M3) {
-    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
-        : "=r"(lo), "=r"(hi)
-        : "r"(w));
-  } else {  // c + 128 in the mantissa of 1024, less 1152
+    constexpr uint32_t SEL = (uint32_t)I | (uint32_t)(I + 8) << 4 | (uint32_t)(I + 4) << 8 | (uint32_t)(I + 12) << 12;
+    uint32_t p;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(p) : "r"(x), "r"(y), "n"(SEL));
+    return (p * times128) & 0xbf80bf80u;
+  } else {
+    constexpr uint32_t SEL = (uint32_t)I | (uint32_t)I << 4 | (uint32_t)(I + 4) << 8 | (uint32_t)(I + 4) << 12;
+    const uint32_t p = (__byte_perm(x, y, SEL) & 0x00ff00ffu) ^ 0x64806480u;
+    const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&p), __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480)));
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+}
+template <int FMT>
+constexpr int kCodeUnit = FMT == TA_CACHE_E4M3 ? 8 : 0;  // fp16 operands are the codes times 2^-kCodeUnit
+// the four codes of a word of a key row, as pairs (0, 1) and (2, 3)
+template <int FMT>
+__device__ __forceinline__ void expand(uint32_t w, uint32_t& lo, uint32_t& hi, uint32_t times128) {
+  if constexpr (FMT == TA_CACHE_E4M3) {  // (the permute takes the bytes where they are)
+    uint32_t p, q;
+    asm("prmt.b32 %0, %1, %1, 0x9180;" : "=r"(p) : "r"(w));
+    asm("prmt.b32 %0, %1, %1, 0xb3a2;" : "=r"(q) : "r"(w));
+    lo = (p * times128) & 0xbf80bf80u;
+    hi = (q * times128) & 0xbf80bf80u;
+  } else {
     const uint32_t u = w ^ 0x80808080u;
-    const uint32_t a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
+    const uint32_t p = __byte_perm(u, 0x64646464u, 0x4140), q = __byte_perm(u, 0x64646464u, 0x4342);
     const __half2 off = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));
-    const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&a), off), y = __hsub2(*reinterpret_cast<const __half2*>(&b), off);
+    const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&p), off), y = __hsub2(*reinterpret_cast<const __half2*>(&q), off);
     lo = *reinterpret_cast<const uint32_t*>(&x);
     hi = *reinterpret_cast<const uint32_t*>(&y);
   }
@@ -171,8 +195,8 @@ __device__ __forceinline__ float joined_max(const float2* ml, int parts, long lo
 
 // blockIdx.x = (unit * row blocks + block) * pieces + piece
 template <int D, int FMT, int MB>
-__global__ void __launch_bounds__(kThreads) ta_attend_kernel(ta_attend_args a, Scratch sc, int pieces, int piece, int row_blocks,
-                                                              ta_dev_status* status) {
+__global__ void __launch_bounds__(kThreads, (FMT != TA_CACHE_BF16 && MB < 2) ? 3 : 2) ta_attend_kernel(ta_attend_args a, Scratch sc, int pieces, int piece, int row_blocks,
+                                                              uint32_t times128, ta_dev_status* status) {
   using S = Shape<D, FMT>;
   constexpr bool CODES = S::CODES, NARROW = MB == 0;
   constexpr int TK = S::TK, NT = TK / 8, KS = S::KS, R = rows_of(MB), MBN = NARROW ? 1 : MB, NR = NARROW ? 1 : 2 * MB;
@@ -181,14 +205,13 @@ __global__ void __launch_bounds__(kThreads) ta_attend_kernel(ta_attend_args a, S
   constexpr int join_bytes = kWarps * R * (D + 4) * 4;
   uint8_t* s_at = smem + (S::RING > join_bytes ? S::RING : join_bytes);
   float* s_q = reinterpret_cast<float*>(s_at);
-  s_at += R * D * 4;
   uint4* s_frag = reinterpret_cast<uint4*>(s_at);  // [hi, lo][mb][ks][lane]
-  s_at += NARROW ? 0 : 2 * MB * KS * 512;
+  s_at += R * D * 4;
   float* s_factor = reinterpret_cast<float*>(s_at);
   int* s_limit = reinterpret_cast<int*>(s_factor + R);
   float2* s_ml = reinterpret_cast<float2*>(s_limit + R);
   uint32_t* s_there = reinterpret_cast<uint32_t*>(s_ml + kWarps * R);
-  int* s_last = reinterpret_cast<int*>(s_there + kWarps * kStages);
+  int* s_last = reinterpret_cast<int*>(s_there + kWarps * S::STAGES);
 
   ta_wait_for_prior_grid();
   const ta_cache_dev& c = a.cache;
@@ -203,43 +226,47 @@ __global__ void __launch_bounds__(kThreads) ta_attend_kernel(ta_attend_args a, S
   const int tiles = (end - begin + TK - 1) / TK, mine = tiles > warp ? (tiles - warp + kWarps - 1) / kWarps : 0;
 
   // ---- the ring
-  const long long base = u.l * c.sl + u.g * c.sh, sbase = u.l * c.ssl + u.g * c.ssh;
-  const uint32_t ring = smem_u32(smem) + warp * kStages * S::STAGE;
-  uint32_t* there_w = s_there + warp * kStages;
-  ta_row_at at = {-1, 0};
-  auto look_up = [&](int i) {  // this lane's row of the warp's i-th tile
+  const uint8_t *k_base = c.k + u.l * c.sl + u.g * c.sh, *v_base = c.v + u.l * c.sl + u.g * c.sh;
+  const uint32_t sp16 = (uint32_t)(c.sp >> 4), sr16 = (uint32_t)(c.sr >> 4);
+  const uint32_t ring = smem_u32(smem) + warp * S::STAGES * S::STAGE;
+  uint32_t* there_w = s_there + warp * S::STAGES;
+  uint32_t at_row = 0, at_scale = 0;  // this lane's row of the next tile, in units of 16 bytes, and its scale
+  bool at_there = false;
+  auto look_up = [&](int i) {
     const int r = begin + (warp + i * kWarps) * TK + lane;
-    at = {-1, 0};
-    if (lane < TK && r < end) {
-      at = ta_cache_row(c, u.b, r);
-      if (at.row < 0) ta_report_bounds(status, 33, u.b, r);
+    at_there = lane < TK && r < end;
+    if (at_there) {
+      const int j = c.page_shift >= 0 ? r >> c.page_shift : (int)((unsigned)r / (unsigned)c.page), in_page = r - j * c.page;
+      const int id = c.table ? c.table[u.b * (long long)c.wide + j] : u.b * c.wide + j;
+      at_there = id >= 0 && id < c.n_pages;
+      if (!at_there) ta_report_bounds(status, 33, u.b, r);
+      at_row = (uint32_t)id * sp16 + (uint32_t)in_page * sr16;
+      at_scale = (uint32_t)id * (uint32_t)c.ssp + (uint32_t)in_page * (uint32_t)c.ssr;
     }
   };
   auto issue = [&](int i) {
     if (i < mine) {
-      const int stage = i % kStages;
+      const int stage = i % S::STAGES;
       const uint32_t dst = ring + stage * S::STAGE;
-      const uint32_t there = __ballot_sync(0xffffffffu, at.row >= 0);
+      const uint32_t there = __ballot_sync(0xffffffffu, at_there);
       if (lane == 0) there_w[stage] = there;
 #pragma unroll
       for (int k = 0; k < TK * S::CHUNKS / 32; ++k) {
         const int row = (k * 32 + lane) / S::CHUNKS, ch = (k * 32 + lane) % S::CHUNKS;
-        const long long off = __shfl_sync(0xffffffffu, at.row, row);
-        const bool is = (there >> row) & 1;
-        const long long src = is ? base + off + ch * 16 : 0;
+        const long long off = (long long)__shfl_sync(0xffffffffu, at_there ? at_row : 0u, row) * 16 + ch * 16;
+        const bool is = (there >> row) & 1;  // (a row that is not there stands at the pool's start and is not read)
         // swizzles: eight lanes that read 16 bytes each at a time meet all banks (keys: two rows and four chunks; values: eight
         // rows of one chunk through ldmatrix, or, of codes, four even rows and two chunks)
         const int kx = S::CHUNKS >= 8 ? (row & 1) << 2 : 0;
         const int vx = !CODES ? row & 7 : S::CHUNKS >= 8 ? ((row >> 1) & 3) << 1 : (row >> 1) & 3;
-        cp16(dst + row * S::ROW + ((ch ^ kx) << 4), c.k + src, is);
-        cp16(dst + S::TILE + row * S::ROW + ((ch ^ vx) << 4), c.v + src, is);
+        cp16(dst + row * S::ROW + ((ch ^ kx) << 4), k_base + off, is);
+        cp16(dst + S::TILE + row * S::ROW + ((ch ^ vx) << 4), v_base + off, is);
       }
       if constexpr (CODES) {
-        const bool is = at.row >= 0;
-        const long long src = is ? sbase + at.scale : 0;
         if (lane < TK) {
-          cp4(dst + 2 * S::TILE + lane * 4, c.ks + src, is);
-          cp4(dst + 2 * S::TILE + TK * 4 + lane * 4, c.vs + src, is);
+          const long long src = u.l * c.ssl + u.g * c.ssh + (at_there ? at_scale : 0u);
+          cp4(dst + 2 * S::TILE + lane * 4, c.ks + src, at_there);
+          cp4(dst + 2 * S::TILE + TK * 4 + lane * 4, c.vs + src, at_there);
         }
       }
       look_up(i + 1);
@@ -248,7 +275,7 @@ __global__ void __launch_bounds__(kThreads) ta_attend_kernel(ta_attend_args a, S
   };
   look_up(0);
 #pragma unroll
-  for (int i = 0; i < kStages - 1; ++i) issue(i);
+  for (int i = 0; i < S::STAGES - 1; ++i) issue(i);
 
   // ---- the queries: fp32 in shared memory, rotated, then fragments
   for (int w = tid; w < R * D; w += kThreads) {
@@ -279,7 +306,7 @@ __global__ void __launch_bounds__(kThreads) ta_attend_kernel(ta_attend_args a, S
   __syncthreads();
   // a row's part of four coordinates for product ks: the order in which a lane's bytes of a key row come
   auto coordinate = [&](int ks) { return CODES ? (t4 + 4 * (ks / 4)) * 16 + (ks % 4) * 4 : (t4 + 4 * (ks / 2)) * 8 + (ks % 2) * 4; };
-  const float bits = a.scale * 1.4426950408889634f;
+  const float bits = a.scale * 1.4426950408889634f * pow2(kCodeUnit<FMT>);
   auto row_scale = [&](int r, float& down) {  // 8-bit caches: a power of two that brings the row's largest value into [1, 2)
     float m = 0.0f;
     if constexpr (CODES) {
@@ -311,27 +338,37 @@ __global__ void __launch_bounds__(kThreads) ta_attend_kernel(ta_attend_args a, S
       qf[ks][3] = rest2<CODES>(v.z * down, v.w * down, qf[ks][2]);
     }
   } else {
-    for (int mb = warp; mb < MB; mb += kWarps) {
+    constexpr int PER_WARP = KS / kWarps;  // products of a warp, of every 16 rows
+    uint4 hi[MB][PER_WARP], lo[MB][PER_WARP];
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
       float d0, d1;
       const float f0 = row_scale(mb * 16 + g8, d0), f1 = row_scale(mb * 16 + g8 + 8, d1);
-      if (t4 == 0) s_factor[mb * 16 + g8] = f0, s_factor[mb * 16 + g8 + 8] = f1;
+      if (warp == 0 && t4 == 0) s_factor[mb * 16 + g8] = f0, s_factor[mb * 16 + g8 + 8] = f1;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const float4 v = *reinterpret_cast<const float4*>(s_q + (mb * 16 + g8) * D + coordinate(ks));
-        const float4 w = *reinterpret_cast<const float4*>(s_q + (mb * 16 + g8 + 8) * D + coordinate(ks));
-        uint4 hi, lo;
-        hi.x = pack2<CODES>(v.x * d0, v.y * d0);
-        hi.y = pack2<CODES>(w.x * d1, w.y * d1);
-        hi.z = pack2<CODES>(v.z * d0, v.w * d0);
-        hi.w = pack2<CODES>(w.z * d1, w.w * d1);
-        lo.x = rest2<CODES>(v.x * d0, v.y * d0, hi.x);
-        lo.y = rest2<CODES>(w.x * d1, w.y * d1, hi.y);
-        lo.z = rest2<CODES>(v.z * d0, v.w * d0, hi.z);
-        lo.w = rest2<CODES>(w.z * d1, w.w * d1, hi.w);
-        s_frag[(mb * KS + ks) * 32 + lane] = hi;
-        s_frag[((MB + mb) * KS + ks) * 32 + lane] = lo;
+      for (int i = 0; i < PER_WARP; ++i) {
+        const int at = coordinate(warp * PER_WARP + i);
+        const float4 v = *reinterpret_cast<const float4*>(s_q + (mb * 16 + g8) * D + at);
+        const float4 w = *reinterpret_cast<const float4*>(s_q + (mb * 16 + g8 + 8) * D + at);
+        uint4 &h = hi[mb][i], &r = lo[mb][i];
+        h.x = pack2<CODES>(v.x * d0, v.y * d0);
+        h.y = pack2<CODES>(w.x * d1, w.y * d1);
+        h.z = pack2<CODES>(v.z * d0, v.w * d0);
+        h.w = pack2<CODES>(w.z * d1, w.w * d1);
+        r.x = rest2<CODES>(v.x * d0, v.y * d0, h.x);
+        r.y = rest2<CODES>(w.x * d1, w.y * d1, h.y);
+        r.z = rest2<CODES>(v.z * d0, v.w * d0, h.z);
+        r.w = rest2<CODES>(w.z * d1, w.w * d1, h.w);
       }
     }
+    __syncthreads();  // the fragments take the queries' place
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+      for (int i = 0; i < PER_WARP; ++i) {
+        s_frag[(mb * KS + warp * PER_WARP + i) * 32 + lane] = hi[mb][i];
+        s_frag[((MB + mb) * KS + warp * PER_WARP + i) * 32 + lane] = lo[mb][i];
+      }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
@@ -355,10 +392,10 @@ __global__ void __launch_bounds__(kThreads) ta_attend_kernel(ta_attend_args a, S
   int ref = -100;  // 8-bit caches: exponent that the value rows' scales are taken relative to
 
   for (int i = 0; i < mine; ++i) {
-    cp_wait<kStages - 2>();
+    cp_wait<S::STAGES - 2>();
     __syncwarp();
-    issue(i + kStages - 1);
-    const int stage = i % kStages, first = begin + (warp + i * kWarps) * TK;
+    issue(i + S::STAGES - 1);
+    const int stage = i % S::STAGES, first = begin + (warp + i * kWarps) * TK;
     const uint32_t kt = ring + stage * S::STAGE, vt = kt + S::TILE, st = kt + 2 * S::TILE;
     const uint32_t there = there_w[stage];
     const bool whole = there == (TK == 32 ? 0xffffffffu : (1u << TK) - 1) && first + TK <= seen_by_all;
@@ -386,7 +423,7 @@ __global__ void __launch_bounds__(kThreads) ta_attend_kernel(ta_attend_args a, S
 #pragma unroll
         for (int y = 0; y < NT; ++y) {
           const uint32_t* wy = reinterpret_cast<const uint32_t*>(&w[y]);
-          if constexpr (CODES) expand<FMT>(wy[h], b0[y], b1[y]);
+          if constexpr (CODES) expand<FMT>(wy[h], b0[y], b1[y], times128);
           else b0[y] = wy[2 * h], b1[y] = wy[2 * h + 1];
         }
         if constexpr (NARROW) {
@@ -499,8 +536,13 @@ __global__ void __launch_bounds__(kThreads) ta_attend_kernel(ta_attend_args a, S
         vs[y].y *= up;
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
-          x[r][y][0] = !whole && x[r][y][0] == 0.0f ? 0.0f : x[r][y][0] * vs[y].x;  // (a scale that is not seen may be NaN)
-          x[r][y][1] = !whole && x[r][y][1] == 0.0f ? 0.0f : x[r][y][1] * vs[y].y;
+          if (whole) {
+            x[r][y][0] *= vs[y].x;
+            x[r][y][1] *= vs[y].y;
+          } else {  // a scale that is not seen may be NaN
+            x[r][y][0] = x[r][y][0] == 0.0f ? 0.0f : x[r][y][0] * vs[y].x;
+            x[r][y][1] = x[r][y][1] == 0.0f ? 0.0f : x[r][y][1] * vs[y].y;
+          }
         }
       }
     }
@@ -520,7 +562,7 @@ __global__ void __launch_bounds__(kThreads) ta_attend_kernel(ta_attend_args a, S
     // ---- values. Rows that a later token sees and an earlier one does not meet probabilities of zero; where such a row is
     // not finite, every token's rows are taken by themselves.
     bool apart = false;
-    if (first + TK > seen_by_all && seen_by_all < end) {
+    if (!CODES && first + TK > seen_by_all && seen_by_all < end) {  // (codes are finite, and scales were dealt with)
       bool bad = false;
       for (int w = lane; w < TK * S::CHUNKS; w += 32) {
         const int row = w / S::CHUNKS;
@@ -529,10 +571,7 @@ __global__ void __launch_bounds__(kThreads) ta_attend_kernel(ta_attend_args a, S
         const uint32_t* p = reinterpret_cast<const uint32_t*>(&v);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          if constexpr (FMT == TA_CACHE_BF16) bad |= (p[k] & 0x7f80u) == 0x7f80u || (p[k] & 0x7f800000u) == 0x7f800000u;
-          else if constexpr (FMT == TA_CACHE_E4M3)
-            bad |= (p[k] & 0x7fu) == 0x7fu || (p[k] & 0x7f00u) == 0x7f00u || (p[k] & 0x7f0000u) == 0x7f0000u ||
-                   (p[k] & 0x7f000000u) == 0x7f000000u;
+          bad |= (p[k] & 0x7f80u) == 0x7f80u || (p[k] & 0x7f800000u) == 0x7f800000u;
         }
       }
       apart = __any_sync(0xffffffffu, bad);
@@ -613,10 +652,10 @@ __global__ void __launch_bounds__(kThreads) ta_attend_kernel(ta_attend_args a, S
 #pragma unroll
         for (int w = 0; w < W; ++w) {
           uint32_t b0[4], b1[4];  // pairs of two rows, one coordinate each
-          expand<FMT>(__byte_perm(v[0][w], v[1][w], 0x5140), b0[0], b0[1]);
-          expand<FMT>(__byte_perm(v[0][w], v[1][w], 0x7362), b0[2], b0[3]);
-          expand<FMT>(__byte_perm(v[2][w], v[3][w], 0x5140), b1[0], b1[1]);
-          expand<FMT>(__byte_perm(v[2][w], v[3][w], 0x7362), b1[2], b1[3]);
+          b0[0] = pair_of<FMT, 0>(v[0][w], v[1][w], times128), b0[1] = pair_of<FMT, 1>(v[0][w], v[1][w], times128);
+          b0[2] = pair_of<FMT, 2>(v[0][w], v[1][w], times128), b0[3] = pair_of<FMT, 3>(v[0][w], v[1][w], times128);
+          b1[0] = pair_of<FMT, 0>(v[2][w], v[3][w], times128), b1[1] = pair_of<FMT, 1>(v[2][w], v[3][w], times128);
+          b1[2] = pair_of<FMT, 2>(v[2][w], v[3][w], times128), b1[3] = pair_of<FMT, 3>(v[2][w], v[3][w], times128);
 #pragma unroll
           for (int e = 0; e < 4; ++e) product(4 * w + e, b0[e], b1[e]);
         }
@@ -629,7 +668,7 @@ __global__ void __launch_bounds__(kThreads) ta_attend_kernel(ta_attend_args a, S
   __syncthreads();  // the rings are free
   constexpr int LD = D + 4;
   float* s_o = reinterpret_cast<float*>(smem);
-  const float unit_of_o = CODES ? pow2(max(ref - 14, -126)) : 1.0f;
+  const float unit_of_o = CODES ? pow2(max(ref - 14 + kCodeUnit<FMT>, -126)) : 1.0f;
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
     l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
@@ -744,22 +783,33 @@ __global__ void __launch_bounds__(256) ta_attend_mass_kernel(ta_attend_args a, S
   }
 }
 
-// How a call is cut: query rows of a block, and pieces of the cache rows. Sized for the 148 SMs of a B200 at two blocks each.
+// How a call is cut: query rows of a block, and pieces of the cache rows. Sized for the 148 SMs of a B200 at two (bf16, or 32
+// query rows) or three blocks each.
 struct Plan {
   int mb, row_blocks, piece, pieces;
 };
-constexpr int kSlots = 2 * 148;
 constexpr int kPieceUnit = 128;  // rows: whole rounds of every variant's four warps
-Plan plan_of(long long units, int rows, int max_len) {
+// The smallest number of pieces that fills whole rounds of resident blocks: a last round with few blocks costs as much as a full
+// one. bf16 is bound by memory and content with 85 % of a round, the 8-bit formats by instructions (95 %). us at 1, 2, 3, 4, 6, 8
+// pieces: 128 units of 32768 bf16 rows 563, 333, 441, 343, 349, 354; 288 units of 16384 e4m3 rows -, 312, 252, 257, 265, -.
+// With more units than fit at once lengths may differ: four rounds at least (512 units of 2048 to 16384 e4m3 rows
+// -, 331, 312, 293, 294, -; 296 units of 32768 bf16 rows alike lose 1.5 %, 726 to 737).
+Plan plan_of(long long units, int rows, int max_len, bool codes) {
   Plan p;
   p.mb = rows <= 8 ? 0 : rows <= 16 ? 1 : 2;
   p.row_blocks = (rows + rows_of(p.mb) - 1) / rows_of(p.mb);
-  const long long groups = units * p.row_blocks;
-  long long want = groups > kAttendTickets ? 1 : (kSlots + groups - 1) / groups;
-  p.piece = (int)(((max_len + want - 1) / want + kPieceUnit - 1) / kPieceUnit * kPieceUnit);
+  const long long groups = units * p.row_blocks, slots = 148 * (codes && p.mb < 2 ? 3 : 2);
+  const int most = groups > kAttendTickets ? 1 : max_len <= kPieceUnit ? 1 : (max_len + kPieceUnit - 1) / kPieceUnit;
+  int k = 1;
+  for (; k < most; ++k) {
+    const long long blocks = groups * k, rounds = (blocks + slots - 1) / slots;
+    if (groups > slots && rounds < 4 && k < 4) continue;
+    if (blocks * 100 >= rounds * slots * (codes ? 95 : 85)) break;
+    if (rounds > 8) break;
+  }
+  p.piece = ((max_len + k - 1) / k + kPieceUnit - 1) / kPieceUnit * kPieceUnit;
   if (p.piece < kPieceUnit) p.piece = kPieceUnit;
-  p.pieces = (max_len + p.piece - 1) / p.piece;
-  if (p.pieces < 1) p.pieces = 1;
+  p.pieces = max_len > p.piece ? (max_len + p.piece - 1) / p.piece : 1;
   return p;
 }
 constexpr size_t up(size_t x) { return (x + 255) / 256 * 256; }
@@ -777,7 +827,7 @@ cudaError_t launch(const ta_attend_args& a, const Scratch& sc, const Plan& p, cu
     set[dev & 63] = true;
   }
   cfg.dynamicSmemBytes = smem;
-  return cudaLaunchKernelEx(&cfg, ta_attend_kernel<D, FMT, MB>, a, sc, p.pieces, p.piece, p.row_blocks, status);
+  return cudaLaunchKernelEx(&cfg, ta_attend_kernel<D, FMT, MB>, a, sc, p.pieces, p.piece, p.row_blocks, 128u, status);
 }
 template <int D, int FMT>
 cudaError_t launch(const ta_attend_args& a, const Scratch& sc, const Plan& p, cudaLaunchConfig_t& cfg, ta_dev_status* status) {
@@ -792,8 +842,8 @@ cudaError_t launch(const ta_attend_args& a, const Scratch& sc, const Plan& p, cu
   return launch<D, TA_CACHE_INT8>(a, sc, p, cfg, status);
 }
 
-size_t carve(long long units, int rows, int d, int max_len, bool with_mass, uint8_t* base, Scratch* sc) {
-  const Plan p = plan_of(units, rows, max_len);
+size_t carve(long long units, int rows, int d, int max_len, bool codes, bool with_mass, uint8_t* base, Scratch* sc) {
+  const Plan p = plan_of(units, rows, max_len, codes);
   const size_t slots = p.pieces > 1 ? (size_t)units * p.row_blocks * p.pieces * rows_of(p.mb) : 0;
   const long long stride = (max_len + 31) / 32 * 32;
   size_t off = 0;
@@ -816,15 +866,16 @@ size_t carve(long long units, int rows, int d, int max_len, bool with_mass, uint
 
 }  // namespace
 
-size_t ta_attend_scratch(int units, int rows, int d, int max_len, bool with_mass) {
-  return carve(units, rows, d, max_len, with_mass, nullptr, nullptr);
+size_t ta_attend_scratch(int units, int rows, int d, int max_len, bool codes, bool with_mass) {
+  return carve(units, rows, d, max_len, codes, with_mass, nullptr, nullptr);
 }
 
 cudaError_t ta_launch_attend(const ta_attend_args& a, int* tickets, ta_dev_status* status, cudaStream_t stream) {
   const int units = a.n_layers * a.cache.batch * a.cache.Hkv, rows = a.Hq / a.cache.Hkv * a.T;
-  const Plan p = plan_of(units, rows, a.max_len);
+  const bool codes = a.cache.format != TA_CACHE_BF16;
+  const Plan p = plan_of(units, rows, a.max_len, codes);
   Scratch sc;
-  carve(units, rows, a.d, a.max_len, a.mass != nullptr, a.scratch, &sc);
+  carve(units, rows, a.d, a.max_len, codes, a.mass != nullptr, a.scratch, &sc);
   sc.ticket = tickets;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((long long)units * p.row_blocks * p.pieces), 1, 1);
