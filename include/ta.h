@@ -539,7 +539,8 @@ typedef struct ta_cache {
 
 /* Writes the keys and values of batch->n_layers (= cache->n_layers) layers' new tokens into the cache.
  *   k, v    bf16 views, positions = new tokens, heads = Hkv; ragged where the batch is
- *   rotary  rotates the keys on their way (HOST; positions NULL: a token's position is its row), or NULL
+ *   rotary  rotates the keys on their way (HOST), or NULL. positions NULL: a token's position is its row lens + i, which is
+ *           refused with `rows` or lengths per unit
  *   rows    DEVICE int32 [L][B][Hkv][n_uniform], or [L][Hkv][total_tokens] where the batch is ragged: the row of every token,
  *           negative: not written; NULL: token i of a sequence goes to row lens + i. The lengths are not changed.
  * A row of an 8-bit cache: with m the largest magnitude, at least 2^-100, and F = 448 (E4M3) or 127 (INT8), scale = m / F

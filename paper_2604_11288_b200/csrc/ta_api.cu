@@ -1149,6 +1149,7 @@ ta_status check_move(const ta_ctx* ctx, const ta_cache* cache, const ta_batch* b
   if (s == TA_OK) s = check_batch(batch);
   if (s != TA_OK) return s;
   if (batch->n_layers != cache->n_layers || batch->batch != cache->batch) return TA_ERR_INVALID_ARG;
+  if (batch->total_tokens * cache->Hkv > 0x7fffffffLL) return TA_ERR_UNSUPPORTED;
   s = check_view(k, batch->cu_seqlens == nullptr, cache->d);
   return s == TA_OK ? check_view(v, batch->cu_seqlens == nullptr, cache->d) : s;
 }
@@ -1235,6 +1236,8 @@ ta_status ta_cache_append(ta_ctx* ctx, const ta_cache* cache, const ta_batch* ba
   ta_status s = check_move(ctx, cache, batch, k, v);
   if (s == TA_OK && rotary) s = check_rotary(rotary, cache->d);
   if (s != TA_OK) return s;
+  // a row is a position where it is the same for all layers and heads
+  if (rotary && !rotary->positions && (rows || (cache->lens && cache->lens_per_unit))) return TA_ERR_INVALID_ARG;
   DeviceGuard guard(ctx->device);
   ta_cache_move_args a = move_args(*cache, *batch, k, v, rows);
   a.rot = rotary_dev(rotary);

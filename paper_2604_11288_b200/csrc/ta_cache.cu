@@ -1,26 +1,39 @@
 // Writing new keys and values into a cache, in its format, and reading rows back.
+//
+// Both move every row once: 2 d bytes of bf16 on one side and 2 d or d + 4 on the other, for a handful of operations an
+// element; memory is the bound. A row is held by d / 8 lanes, 16 bytes of bf16 each (8 of codes), so a warp holds two rows
+// (d = 128) or four; a thread has kRows rows of k and of v on their way at once. The largest magnitude of a row meets in
+// three or four shuffles. Keys that are rotated: the angles of a block's tokens are formed once, for all heads, in shared memory;
+// a lane's partner coordinates (half layout) come by shuffles.
 #include "ta_cache.cuh"
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
+constexpr int kThreads = 128;
+constexpr int kItems = 32;  // rows of k, and of v, of a block
 
 struct Token {
   int b, i;  // sequence and index in it
 };
-__device__ __forceinline__ Token token_of(const ta_seq_desc& seq, long long tok) {
+// The sequence of a token, looked for by a whole warp: 32 offsets at a time, not one after another.
+__device__ __forceinline__ int sequence_of(const ta_seq_desc& seq, long long tok) {
+  const int lane = threadIdx.x & 31;
+  int b = -1;
+  for (int at = 0; at < seq.batch; at += 32) {  // the last sequence that begins at or before the token
+    const int n = __popc(__ballot_sync(0xffffffffu, at + lane < seq.batch && seq.cu[at + lane] <= tok));
+    b += n;
+    if (n < 32) break;
+  }
+  return max(b, 0);
+}
+// Token tok of the batch; b0: the sequence of a token shortly before it.
+__device__ __forceinline__ Token token_of(const ta_seq_desc& seq, long long tok, int b0) {
   if (!seq.cu) {
-    const int b = (int)(tok / seq.n_uniform);
+    const int b = (int)((unsigned)tok / (unsigned)seq.n_uniform);
     return {b, (int)(tok - (long long)b * seq.n_uniform)};
   }
-  int lo = 0, hi = seq.batch;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (seq.cu[mid] <= tok) lo = mid;
-    else hi = mid;
-  }
-  return {lo, (int)(tok - seq.cu[lo])};
+  while (b0 + 1 < seq.batch && seq.cu[b0 + 1] <= tok) ++b0;
+  return {b0, (int)(tok - seq.cu[b0])};
 }
 __device__ __forceinline__ long long view_at(const ta_bf16_view& v, const ta_seq_desc& seq, int l, int g, Token t, long long tok) {
   return l * v.stride_l + g * v.stride_h + (seq.cu ? tok * v.stride_n : t.b * v.stride_b + t.i * v.stride_n);
@@ -29,144 +42,329 @@ __device__ __forceinline__ long long view_at(const ta_bf16_view& v, const ta_seq
 __device__ __forceinline__ long long rows_at(const ta_seq_desc& seq, int Hkv, int l, int g, Token t, long long tok) {
   return seq.cu ? ((long long)l * Hkv + g) * seq.total + tok : (((long long)l * seq.batch + t.b) * Hkv + g) * seq.n_uniform + t.i;
 }
+__device__ __forceinline__ float2 both(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint4 load16(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ uint2 load8(const void* p) {
+  uint2 v;
+  asm volatile("ld.global.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 x, y;\n\tcvt.rn.satfinite.e4m3x2.f32 x, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 y, %4, %3;\n\tmov.b32 %0, {x, y};\n\t}"
+      : "=r"(r)
+      : "f"(a), "f"(b), "f"(c), "f"(d));
+  return r;
+}
+// whole numbers -127..127 to nearest even: added to 1.5 * 2^23 they stand in the mantissa's lowest byte
+__device__ __forceinline__ uint32_t int8x4(float a, float b, float c, float d) {
+  constexpr float M = 12582912.0f;
+  const uint32_t x = __float_as_uint(__fadd_rn(a, M)), y = __float_as_uint(__fadd_rn(b, M));
+  const uint32_t z = __float_as_uint(__fadd_rn(c, M)), w = __float_as_uint(__fadd_rn(d, M));
+  return __byte_perm(__byte_perm(x, y, 0x0040), __byte_perm(z, w, 0x0040), 0x5410);
+}
 
-// A warp per row of k and of v: lane j holds coordinates j, j + 32, ...
+struct Place {  // of an item: a token's row of one head
+  long long k, v;        // offsets in the views
+  long long row, scale;  // offsets in the cache's rows (bytes; -1: there is none) and scales
+};
+
+// What a lane has of a row: coordinates 8 lane .. 8 lane + 7. A group of D / 8 lanes takes a row at a time.
 template <int D>
+struct Lanes {
+  static constexpr int N = D / 8, GROUPS = kThreads / N;
+};
+
+// Items are counted token * Hkv + head. grid.x = kItems of them, grid.y = layers.
+template <int D, int FMT, bool TURN>
 __global__ void __launch_bounds__(kThreads) ta_cache_append_kernel(ta_cache_move_args a, ta_dev_status* status) {
   ta_wait_for_prior_grid();
-  constexpr int N = D / 32;
-  __shared__ float s_row[kWarps][D];
+  constexpr int N = Lanes<D>::N, GROUPS = Lanes<D>::GROUPS, PER = kItems / GROUPS;
+  constexpr bool CODES = FMT != TA_CACHE_BF16;
+  extern __shared__ float2 s_cs[];  // [token][pair]
+  __shared__ Place s_place[kItems];
   const ta_cache_dev& c = a.cache;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const long long w = (long long)blockIdx.x * kWarps + warp;
-  const int l = blockIdx.y;
-  if (w >= a.seq.total * c.Hkv) return;
-  const long long tok = w / c.Hkv;
-  const int g = (int)(w - tok * c.Hkv);
-  const Token t = token_of(a.seq, tok);
-  const long long row = a.rows ? a.rows[rows_at(a.seq, c.Hkv, l, g, t, tok)] : (long long)ta_cache_len(c, l, t.b, g) + t.i;
-  if (row < 0) {
-    if (!a.rows && lane == 0) ta_report_bounds(status, 30, t.b, (int)row);
-    return;
+  const int lane = threadIdx.x % N, group = threadIdx.x / N, l = blockIdx.y, half = a.rot.d_rot / 2;
+  const unsigned first = blockIdx.x * kItems, todo = min((unsigned)kItems, (unsigned)a.seq.total * c.Hkv - first);
+  const unsigned tok0 = first / c.Hkv, tokens = (first + todo - 1) / c.Hkv - tok0 + 1;
+  const int b0 = a.seq.cu ? sequence_of(a.seq, tok0) : 0;
+  // one thread finds an item's places, while the others form the angles
+  if (threadIdx.x < todo) {
+    const unsigned w = first + threadIdx.x, tok = w / c.Hkv;
+    const int g = (int)(w - tok * c.Hkv);
+    const Token t = token_of(a.seq, tok, b0);
+    Place p;
+    p.k = view_at(a.k, a.seq, l, g, t, tok);
+    p.v = view_at(a.v, a.seq, l, g, t, tok);
+    const long long row = a.rows ? (long long)a.rows[rows_at(a.seq, c.Hkv, l, g, t, tok)] : (long long)ta_cache_len(c, l, t.b, g) + t.i;
+    ta_row_at at = {-1, 0};
+    if (row >= 0 && row < 0x7fffffff) at = ta_cache_row(c, t.b, (int)row);
+    if (at.row < 0 && (row >= 0 || !a.rows)) ta_report_bounds(status, 30, t.b, (int)row);
+    p.row = at.row < 0 ? -1 : l * c.sl + g * c.sh + at.row;
+    p.scale = l * c.ssl + g * c.ssh + at.scale;
+    s_place[threadIdx.x] = p;
   }
-  const ta_row_at at = row < 0x7fffffff ? ta_cache_row(c, t.b, (int)row) : ta_row_at{-1, 0};
-  if (at.row < 0) {
-    if (lane == 0) ta_report_bounds(status, 30, t.b, (int)row);
-    return;
-  }
-  for (int kv = 0; kv < 2; ++kv) {
-    const ta_bf16_view& src = kv ? a.v : a.k;
-    const __nv_bfloat16* x = reinterpret_cast<const __nv_bfloat16*>(src.ptr) + view_at(src, a.seq, l, g, t, tok);
-    uint8_t* dst = (kv ? c.v : c.k) + l * c.sl + g * c.sh + at.row;
-    const bool turned = !kv && a.rot.phase;
-    if (c.format == TA_CACHE_BF16 && !turned) {
-#pragma unroll
-      for (int e = 0; e < N; ++e) reinterpret_cast<__nv_bfloat16*>(dst)[lane + 32 * e] = x[lane + 32 * e];
-      continue;
-    }
-    float f[N];
-#pragma unroll
-    for (int e = 0; e < N; ++e) f[e] = __bfloat162float(x[lane + 32 * e]);
-    if (turned) {
-      const int position = a.rot.positions ? a.rot.positions[tok] : (int)row, half = a.rot.d_rot / 2;
-#pragma unroll
-      for (int e = 0; e < N; ++e) s_row[warp][lane + 32 * e] = f[e];
-      __syncwarp();
-#pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const int j = lane + 32 * e;
-        if (j >= a.rot.d_rot) continue;
-        const bool second = a.rot.interleaved ? (j & 1) : j >= half;
-        const int p = a.rot.interleaved ? j >> 1 : (second ? j - half : j);
-        const int other = a.rot.interleaved ? j ^ 1 : (second ? j - half : j + half);
-        const float2 cs = ta_cos_sin(a.rot, a.rot.phase[p], position);
-        const float o = s_row[warp][other];
-        f[e] = second ? o * cs.y + f[e] * cs.x : f[e] * cs.x - o * cs.y;
+  if constexpr (TURN) {
+    for (unsigned w = kThreads - 1 - threadIdx.x; w < tokens * half; w += kThreads) {
+      const unsigned i = w / half, p = w - i * half, tok = tok0 + i;
+      int position;
+      if (a.rot.positions) {
+        position = a.rot.positions[tok];
+      } else {
+        const Token t = token_of(a.seq, tok, b0);  // the row, the same for all layers and heads
+        position = ta_cache_len(c, l, t.b, 0) + t.i;
       }
-      __syncwarp();
+      s_cs[w] = ta_cos_sin(a.rot, a.rot.phase[p], position);
     }
-    if (c.format == TA_CACHE_BF16) {
+  }
+  __syncthreads();
+  uint4 k[PER], v[PER];
 #pragma unroll
-      for (int e = 0; e < N; ++e) reinterpret_cast<__nv_bfloat16*>(dst)[lane + 32 * e] = __float2bfloat16(f[e]);
-      continue;
+  for (int i = 0; i < PER; ++i) {
+    const int w = group + i * GROUPS;
+    if (w < todo) {
+      k[i] = load16(reinterpret_cast<const __nv_bfloat16*>(a.k.ptr) + s_place[w].k + lane * 8);
+      v[i] = load16(reinterpret_cast<const __nv_bfloat16*>(a.v.ptr) + s_place[w].v + lane * 8);
     }
-    float m = 0x1p-100f;
-    bool bad = false;
+  }
+  // the row's coordinates of this lane, rotated
+  auto turn = [&](float (&f)[8], int w) {
+    const float2* cs = s_cs + ((first + w) / c.Hkv - tok0) * half;
+    if (a.rot.interleaved) {
+      if (lane * 8 < a.rot.d_rot) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      m = fmaxf(m, fabsf(f[e]));
-      bad = bad || !(fabsf(f[e]) <= 3.402823466e38f);
+        for (int e = 0; e < 4; ++e) {
+          const float2 r = cs[lane * 4 + e];
+          const float x = f[2 * e], y = f[2 * e + 1];
+          f[2 * e] = x * r.x - y * r.y;
+          f[2 * e + 1] = x * r.y + y * r.x;
+        }
+      }
+    } else {  // partners are `half` coordinates away: a multiple of 4
+      float o[8];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {  // four coordinates of one side
+        const int at = lane * 8 + 4 * q, other = at < half ? at + half : at - half;
+        const bool upper = (other & 4) != 0;  // the partners are a lane's upper four
+        const int from = (threadIdx.x & 31) - lane + ((other >> 3) & (N - 1));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float lo = __shfl_sync(0xffffffffu, f[e], from), hi = __shfl_sync(0xffffffffu, f[4 + e], from);
+          o[4 * q + e] = upper ? hi : lo;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int at = lane * 8 + e;
+        if (at >= a.rot.d_rot) continue;
+        const float2 r = cs[at < half ? at : at - half];
+        f[e] = at < half ? f[e] * r.x - o[e] * r.y : o[e] * r.y + f[e] * r.x;
+      }
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    bad = __any_sync(0xffffffffu, bad);
-    const float full = c.format == TA_CACHE_E4M3 ? 448.0f : 127.0f;
-    const float inv = bad ? 0.0f : __fdiv_rn(full, m);
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const float y = bad ? 0.0f : f[e] * inv;
-      if (c.format == TA_CACHE_E4M3) dst[lane + 32 * e] = __nv_cvt_float_to_fp8(y, __NV_SATFINITE, __NV_E4M3);
-      else reinterpret_cast<int8_t*>(dst)[lane + 32 * e] = (int8_t)__float2int_rn(y);
+  };
+  auto put = [&](const uint4& x, int w, bool is, bool turned, uint8_t* rows, float* scales) {
+    const long long row = is ? s_place[w].row : -1;
+    uint8_t* dst = rows + row;
+    if (!CODES && !turned) {
+      if (row >= 0) *reinterpret_cast<uint4*>(dst + lane * 16) = x;
+      return;
     }
-    if (lane == 0) (kv ? c.vs : c.ks)[l * c.ssl + g * c.ssh + at.scale] = bad ? __int_as_float(0x7fc00000) : __fdiv_rn(m, full);
+    float f[8];
+    const uint32_t word[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 p = both(word[e]);
+      f[2 * e] = p.x;
+      f[2 * e + 1] = p.y;
+    }
+    if (turned) turn(f, w);
+    if constexpr (!CODES) {
+      if (row >= 0)
+        *reinterpret_cast<uint4*>(dst + lane * 16) = make_uint4(pack(f[0], f[1]), pack(f[2], f[3]), pack(f[4], f[5]), pack(f[6], f[7]));
+    } else {
+      // the largest magnitude, as bits: those of infinities and NaN are the largest of all
+      uint32_t top = __float_as_uint(0x1p-100f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[e]) & 0x7fffffffu);
+#pragma unroll
+      for (int o = N / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const bool bad = top >= 0x7f800000u;
+      constexpr float FULL = FMT == TA_CACHE_E4M3 ? 448.0f : 127.0f;
+      const float m = __uint_as_float(top), inv = __fdiv_rn(FULL, m);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = bad ? 0.0f : f[e] * inv;
+      uint2 code;
+      if constexpr (FMT == TA_CACHE_E4M3) code = make_uint2(e4m3x4(f[0], f[1], f[2], f[3]), e4m3x4(f[4], f[5], f[6], f[7]));
+      else code = make_uint2(int8x4(f[0], f[1], f[2], f[3]), int8x4(f[4], f[5], f[6], f[7]));
+      if (row >= 0) {
+        *reinterpret_cast<uint2*>(dst + lane * 8) = code;
+        if (lane == 0) scales[s_place[w].scale] = bad ? __int_as_float(0x7fc00000) : __fdiv_rn(m, FULL);
+      }
+    }
+  };
+
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    if (i * GROUPS >= todo) break;  // (the same for all lanes of a warp: shuffles)
+    const bool is = group + i * GROUPS < todo;  // a group without an item goes along and writes nothing
+    const int w = is ? group + i * GROUPS : 0;
+    if (!is) k[i] = v[i] = make_uint4(0u, 0u, 0u, 0u);
+    put(k[i], w, is, TURN, c.k, c.ks);
+    put(v[i], w, is, false, c.v, c.vs);
   }
 }
 
-template <int D>
+// Items in the order [B][Hkv][n], or [Hkv][total] where the batch is ragged. grid.x = kItems of them, grid.y = layers.
+template <int D, int FMT>
 __global__ void __launch_bounds__(kThreads) ta_cache_read_kernel(ta_cache_move_args a, ta_dev_status* status) {
   ta_wait_for_prior_grid();
-  constexpr int N = D / 32;
+  constexpr int N = Lanes<D>::N, GROUPS = Lanes<D>::GROUPS, PER = kItems / GROUPS;
+  constexpr bool CODES = FMT != TA_CACHE_BF16;
+  __shared__ Place s_place[kItems];
+  __shared__ float2 s_scale[kItems];
   const ta_cache_dev& c = a.cache;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const long long w = (long long)blockIdx.x * kWarps + warp;
-  const int l = blockIdx.y;
-  if (w >= a.seq.total * c.Hkv) return;
-  const long long tok = w / c.Hkv;
-  const int g = (int)(w - tok * c.Hkv);
-  const Token t = token_of(a.seq, tok);
-  const int row = a.rows ? a.rows[rows_at(a.seq, c.Hkv, l, g, t, tok)] : t.i;
-  const ta_row_at at = row >= 0 ? ta_cache_row(c, t.b, row) : ta_row_at{-1, 0};
-  if (row >= 0 && at.row < 0 && lane == 0) ta_report_bounds(status, 31, t.b, row);
-  for (int kv = 0; kv < 2; ++kv) {
-    const ta_bf16_view& out = kv ? a.v : a.k;
-    __nv_bfloat16* y = reinterpret_cast<__nv_bfloat16*>(const_cast<void*>(out.ptr)) + view_at(out, a.seq, l, g, t, tok);
-    const uint8_t* src = (kv ? c.v : c.k) + l * c.sl + g * c.sh + at.row;
-    const float scale = at.row >= 0 && c.format != TA_CACHE_BF16 ? (kv ? c.vs : c.ks)[l * c.ssl + g * c.ssh + at.scale] : 1.0f;
+  const int lane = threadIdx.x % N, group = threadIdx.x / N, l = blockIdx.y;
+  const unsigned first = blockIdx.x * kItems, todo = min((unsigned)kItems, (unsigned)a.seq.total * c.Hkv - first);
+  if (threadIdx.x < 32) {  // a lane finds an item's places
+    const unsigned w = first + min(threadIdx.x, todo - 1);
+    Token t;
+    int g;
+    unsigned tok = 0;
+    if (a.seq.cu) {
+      g = (int)(w / (unsigned)a.seq.total);
+      tok = w - (unsigned)g * (unsigned)a.seq.total;
+      const unsigned tok0 = __shfl_sync(0xffffffffu, tok, 0);
+      const int b0 = sequence_of(a.seq, tok0);
+      t = token_of(a.seq, tok, tok >= tok0 ? b0 : 0);  // (the next head's tokens begin anew)
+    } else {
+      const unsigned u = w / (unsigned)a.seq.n_uniform;
+      t.i = (int)(w - u * a.seq.n_uniform);
+      t.b = (int)(u / (unsigned)c.Hkv);
+      g = (int)(u - (unsigned)t.b * c.Hkv);
+    }
+    Place p;
+    p.k = view_at(a.k, a.seq, l, g, t, tok);
+    p.v = view_at(a.v, a.seq, l, g, t, tok);
+    const int row = a.rows ? a.rows[rows_at(a.seq, c.Hkv, l, g, t, tok)] : t.i;
+    const ta_row_at at = row >= 0 ? ta_cache_row(c, t.b, row) : ta_row_at{-1, 0};
+    if (row >= 0 && at.row < 0 && threadIdx.x < todo) ta_report_bounds(status, 31, t.b, row);
+    p.row = at.row < 0 ? -1 : l * c.sl + g * c.sh + at.row;
+    s_place[threadIdx.x] = p;
+    if constexpr (CODES) {
+      const long long at_scale = l * c.ssl + g * c.ssh + at.scale;
+      s_scale[threadIdx.x] = at.row < 0 ? make_float2(0.0f, 0.0f) : make_float2(c.ks[at_scale], c.vs[at_scale]);
+    }
+  }
+  __syncthreads();
+  uint4 x[PER][CODES ? 1 : 2];
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const int j = lane + 32 * e;
-      __nv_bfloat16 o = __float2bfloat16(0.0f);
-      if (at.row >= 0) {
-        if (c.format == TA_CACHE_BF16) o = reinterpret_cast<const __nv_bfloat16*>(src)[j];
-        else if (c.format == TA_CACHE_E4M3)
-          o = __float2bfloat16(__half2float(__half(__nv_cvt_fp8_to_halfraw(src[j], __NV_E4M3))) * scale);
-        else o = __float2bfloat16((float)reinterpret_cast<const int8_t*>(src)[j] * scale);
+  for (int k = 0; k < PER; ++k) {
+    const int w = group + k * GROUPS;
+    const long long row = s_place[w].row + lane * (CODES ? 8 : 16);
+    const bool is = w < todo && s_place[w].row >= 0;
+    if constexpr (CODES) {
+      uint2 p = make_uint2(0u, 0u), q = p;
+      if (is) {
+        p = load8(c.k + row);
+        q = load8(c.v + row);
       }
-      y[j] = o;
+      x[k][0] = make_uint4(p.x, p.y, q.x, q.y);
+    } else {
+      x[k][0] = x[k][1] = make_uint4(0u, 0u, 0u, 0u);
+      if (is) {
+        x[k][0] = load16(c.k + row);
+        x[k][1] = load16(c.v + row);
+      }
+    }
+  }
+  auto value = [&](uint32_t w, int e) {  // code e of a word
+    if constexpr (FMT == TA_CACHE_E4M3) {
+      const __half h = __half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)(w >> (8 * e)), __NV_E4M3));
+      return __half2float(h);
+    } else {
+      return (float)(int)(int8_t)(w >> (8 * e));
+    }
+  };
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int w = group + k * GROUPS;
+    if (w >= todo) break;
+    const float2 scales = CODES ? s_scale[w] : make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      uint4 o;
+      if constexpr (CODES) {
+        const uint32_t p = kv ? x[k][0].z : x[k][0].x, q = kv ? x[k][0].w : x[k][0].y;
+        const float s = kv ? scales.y : scales.x;
+        o.x = pack(value(p, 0) * s, value(p, 1) * s);
+        o.y = pack(value(p, 2) * s, value(p, 3) * s);
+        o.z = pack(value(q, 0) * s, value(q, 1) * s);
+        o.w = pack(value(q, 2) * s, value(q, 3) * s);
+      } else {
+        o = x[k][kv];
+      }
+      uint16_t* dst = reinterpret_cast<uint16_t*>(const_cast<void*>(kv ? a.v.ptr : a.k.ptr)) + (kv ? s_place[w].v : s_place[w].k) + lane * 8;
+      ta_st_stream(reinterpret_cast<uint4*>(dst), o);
     }
   }
 }
 
-template <class K>
-cudaError_t launch(K kernel, const ta_cache_move_args& a, ta_dev_status* status, cudaStream_t stream) {
-  const long long rows = a.seq.total * a.cache.Hkv;
-  if (rows == 0) return cudaSuccess;
+cudaLaunchConfig_t config(const ta_cache_move_args& a, cudaStream_t stream, cudaLaunchAttribute* attr) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((rows + kWarps - 1) / kWarps), (unsigned)a.n_layers, 1);
+  cfg.gridDim = dim3((unsigned)((a.seq.total * a.cache.Hkv + kItems - 1) / kItems), (unsigned)a.n_layers, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
   cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  ta_pdl_attribute(&attr[0]);
+  ta_pdl_attribute(attr);
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, a, status);
+  return cfg;
+}
+template <int D, int FMT>
+cudaError_t append(const ta_cache_move_args& a, ta_dev_status* status, cudaStream_t stream) {
+  cudaLaunchAttribute attr[1];
+  cudaLaunchConfig_t cfg = config(a, stream, attr);
+  if (!a.rot.phase) return cudaLaunchKernelEx(&cfg, ta_cache_append_kernel<D, FMT, false>, a, status);
+  const int tokens = (kItems + a.cache.Hkv - 2) / a.cache.Hkv + 1;  // that a block's items may belong to
+  cfg.dynamicSmemBytes = (size_t)tokens * (a.rot.d_rot / 2) * sizeof(float2);
+  return cudaLaunchKernelEx(&cfg, ta_cache_append_kernel<D, FMT, true>, a, status);
+}
+template <int D, int FMT>
+cudaError_t read(const ta_cache_move_args& a, ta_dev_status* status, cudaStream_t stream) {
+  cudaLaunchAttribute attr[1];
+  cudaLaunchConfig_t cfg = config(a, stream, attr);
+  return cudaLaunchKernelEx(&cfg, ta_cache_read_kernel<D, FMT>, a, status);
 }
 
 }  // namespace
 
 cudaError_t ta_launch_cache_append(const ta_cache_move_args& a, ta_dev_status* status, cudaStream_t stream) {
-  return a.d == 64 ? launch(ta_cache_append_kernel<64>, a, status, stream) : launch(ta_cache_append_kernel<128>, a, status, stream);
+  if (a.seq.total == 0) return cudaSuccess;
+  const int f = a.cache.format;
+  if (a.d == 64)
+    return f == TA_CACHE_BF16 ? append<64, TA_CACHE_BF16>(a, status, stream)
+           : f == TA_CACHE_E4M3 ? append<64, TA_CACHE_E4M3>(a, status, stream)
+                                : append<64, TA_CACHE_INT8>(a, status, stream);
+  return f == TA_CACHE_BF16 ? append<128, TA_CACHE_BF16>(a, status, stream)
+         : f == TA_CACHE_E4M3 ? append<128, TA_CACHE_E4M3>(a, status, stream)
+                              : append<128, TA_CACHE_INT8>(a, status, stream);
 }
 cudaError_t ta_launch_cache_read(const ta_cache_move_args& a, ta_dev_status* status, cudaStream_t stream) {
-  return a.d == 64 ? launch(ta_cache_read_kernel<64>, a, status, stream) : launch(ta_cache_read_kernel<128>, a, status, stream);
+  if (a.seq.total == 0) return cudaSuccess;
+  const int f = a.cache.format;
+  if (a.d == 64)
+    return f == TA_CACHE_BF16 ? read<64, TA_CACHE_BF16>(a, status, stream)
+           : f == TA_CACHE_E4M3 ? read<64, TA_CACHE_E4M3>(a, status, stream)
+                                : read<64, TA_CACHE_INT8>(a, status, stream);
+  return f == TA_CACHE_BF16 ? read<128, TA_CACHE_BF16>(a, status, stream)
+         : f == TA_CACHE_E4M3 ? read<128, TA_CACHE_E4M3>(a, status, stream)
+                              : read<128, TA_CACHE_INT8>(a, status, stream);
 }
