@@ -5,6 +5,8 @@
 // (d = 128) or four; a thread has kRows rows of k and of v on their way at once. The largest magnitude of a row meets in
 // three or four shuffles. Keys that are rotated: the angles of a block's tokens are formed once, for all heads, in shared memory;
 // a lane's partner coordinates (half layout) come by shuffles.
+#include <math.h>
+
 #include "ta_cache.cuh"
 
 namespace {
@@ -65,6 +67,11 @@ __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
       : "f"(a), "f"(b), "f"(c), "f"(d));
   return r;
 }
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 // whole numbers -127..127 to nearest even: added to 1.5 * 2^23 they stand in the mantissa's lowest byte
 __device__ __forceinline__ uint32_t int8x4(float a, float b, float c, float d) {
   constexpr float M = 12582912.0f;
@@ -73,9 +80,11 @@ __device__ __forceinline__ uint32_t int8x4(float a, float b, float c, float d) {
   return __byte_perm(__byte_perm(x, y, 0x0040), __byte_perm(z, w, 0x0040), 0x5410);
 }
 
-struct Place {  // of an item: a token's row of one head
-  long long k, v;        // offsets in the views
-  long long row, scale;  // offsets in the cache's rows (bytes; -1: there is none) and scales
+struct Place {  // of an item, a token's row of one head, in the cache
+  long long row, scale;  // offsets of the row (bytes; -1: there is none) and of its scale
+};
+struct Sides {  // of an item in the views
+  long long k, v;
 };
 
 // What a lane has of a row: coordinates 8 lane .. 8 lane + 7. A group of D / 8 lanes takes a row at a time.
@@ -96,15 +105,37 @@ __global__ void __launch_bounds__(kThreads) ta_cache_append_kernel(ta_cache_move
   const int lane = threadIdx.x % N, group = threadIdx.x / N, l = blockIdx.y, half = a.rot.d_rot / 2;
   const unsigned first = blockIdx.x * kItems, todo = min((unsigned)kItems, (unsigned)a.seq.total * c.Hkv - first);
   const unsigned tok0 = first / c.Hkv, tokens = (first + todo - 1) / c.Hkv - tok0 + 1;
+  // a group of lanes has PER items that follow one another: heads of one token, as a rule
+  uint4 k[PER], v[PER];
+  {
+    const unsigned w = first + group * PER;
+    unsigned tok = w / c.Hkv;
+    int g = (int)(w - tok * c.Hkv);
+    const __nv_bfloat16 *kp = nullptr, *vp = nullptr;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if (i == 0 || g == 0) {  // a token's first item here
+        Token t = {0, 0};
+        if (!a.seq.cu) t = token_of(a.seq, tok, 0);
+        kp = reinterpret_cast<const __nv_bfloat16*>(a.k.ptr) + view_at(a.k, a.seq, l, g, t, tok) + lane * 8;
+        vp = reinterpret_cast<const __nv_bfloat16*>(a.v.ptr) + view_at(a.v, a.seq, l, g, t, tok) + lane * 8;
+      }
+      if (group * PER + i < todo) {
+        k[i] = load16(kp);
+        v[i] = load16(vp);
+      }
+      kp += a.k.stride_h;
+      vp += a.v.stride_h;
+      if (++g == c.Hkv) g = 0, ++tok;
+    }
+  }
   const int b0 = a.seq.cu ? sequence_of(a.seq, tok0) : 0;
-  // one thread finds an item's places, while the others form the angles
+  // one thread finds an item's place, while the others form the angles
   if (threadIdx.x < todo) {
     const unsigned w = first + threadIdx.x, tok = w / c.Hkv;
     const int g = (int)(w - tok * c.Hkv);
     const Token t = token_of(a.seq, tok, b0);
     Place p;
-    p.k = view_at(a.k, a.seq, l, g, t, tok);
-    p.v = view_at(a.v, a.seq, l, g, t, tok);
     const long long row = a.rows ? (long long)a.rows[rows_at(a.seq, c.Hkv, l, g, t, tok)] : (long long)ta_cache_len(c, l, t.b, g) + t.i;
     ta_row_at at = {-1, 0};
     if (row >= 0 && row < 0x7fffffff) at = ta_cache_row(c, t.b, (int)row);
@@ -127,58 +158,71 @@ __global__ void __launch_bounds__(kThreads) ta_cache_append_kernel(ta_cache_move
     }
   }
   __syncthreads();
-  uint4 k[PER], v[PER];
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int w = group + i * GROUPS;
-    if (w < todo) {
-      k[i] = load16(reinterpret_cast<const __nv_bfloat16*>(a.k.ptr) + s_place[w].k + lane * 8);
-      v[i] = load16(reinterpret_cast<const __nv_bfloat16*>(a.v.ptr) + s_place[w].v + lane * 8);
-    }
-  }
   // the row's coordinates of this lane, rotated
-  auto turn = [&](float (&f)[8], int w) {
-    const float2* cs = s_cs + ((first + w) / c.Hkv - tok0) * half;
+  float2 cs[8];
+  unsigned of_cs = ~0u;  // the token that they are of
+  auto turn = [&](float (&f)[8], const uint4& x, int w) {
+    const unsigned tok = (first + w) / c.Hkv - tok0;
+    const int at = lane * 8;
     if (a.rot.interleaved) {
-      if (lane * 8 < a.rot.d_rot) {
+      if (at < a.rot.d_rot && tok != of_cs) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) cs[e] = s_cs[tok * half + lane * 4 + e];
+      }
+      if (at < a.rot.d_rot) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float2 r = cs[lane * 4 + e];
-          const float x = f[2 * e], y = f[2 * e + 1];
-          f[2 * e] = x * r.x - y * r.y;
-          f[2 * e + 1] = x * r.y + y * r.x;
+          const float p = f[2 * e], q = f[2 * e + 1];
+          f[2 * e] = p * cs[e].x - q * cs[e].y;
+          f[2 * e + 1] = p * cs[e].y + q * cs[e].x;
         }
       }
     } else {  // partners are `half` coordinates away: a multiple of 4
-      float o[8];
+      const uint32_t word[4] = {x.x, x.y, x.z, x.w};
+      uint32_t o[4];
+      const int leader = (threadIdx.x & 31) - lane;
+      if ((half & 7) == 0) {
+        const int from = leader + (((at < half ? at + half : at - half) >> 3) & (N - 1));
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {  // four coordinates of one side
-        const int at = lane * 8 + 4 * q, other = at < half ? at + half : at - half;
-        const bool upper = (other & 4) != 0;  // the partners are a lane's upper four
-        const int from = (threadIdx.x & 31) - lane + ((other >> 3) & (N - 1));
+        for (int e = 0; e < 4; ++e) o[e] = __shfl_sync(0xffffffffu, word[e], from);
+      } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float lo = __shfl_sync(0xffffffffu, f[e], from), hi = __shfl_sync(0xffffffffu, f[4 + e], from);
-          o[4 * q + e] = upper ? hi : lo;
+        for (int q = 0; q < 2; ++q) {  // four coordinates of one side
+          const int mine = at + 4 * q, other = mine < half ? mine + half : mine - half;
+          const int from = leader + ((other >> 3) & (N - 1));
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t lo = __shfl_sync(0xffffffffu, word[e], from), hi = __shfl_sync(0xffffffffu, word[2 + e], from);
+            o[2 * q + e] = (other & 4) ? hi : lo;  // the partners are a lane's lower or upper four
+          }
         }
       }
+      if (at < a.rot.d_rot) {  // (a multiple of 8)
+        if (tok != of_cs) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int at = lane * 8 + e;
-        if (at >= a.rot.d_rot) continue;
-        const float2 r = cs[at < half ? at : at - half];
-        f[e] = at < half ? f[e] * r.x - o[e] * r.y : o[e] * r.y + f[e] * r.x;
+          for (int q = 0; q < 2; ++q) {
+            const int mine = at + 4 * q;
+            const float4* r = reinterpret_cast<const float4*>(s_cs + tok * half + (mine < half ? mine : mine - half));
+            const float sign = mine < half ? -1.0f : 1.0f;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float4 two = r[e];
+              cs[4 * q + 2 * e] = make_float2(two.x, two.y * sign);
+              cs[4 * q + 2 * e + 1] = make_float2(two.z, two.w * sign);
+            }
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 p = both(o[e]);
+          f[2 * e] = f[2 * e] * cs[2 * e].x + p.x * cs[2 * e].y;
+          f[2 * e + 1] = f[2 * e + 1] * cs[2 * e + 1].x + p.y * cs[2 * e + 1].y;
+        }
       }
     }
+    of_cs = tok;
   };
-  auto put = [&](const uint4& x, int w, bool is, bool turned, uint8_t* rows, float* scales) {
-    const long long row = is ? s_place[w].row : -1;
-    uint8_t* dst = rows + row;
-    if (!CODES && !turned) {
-      if (row >= 0) *reinterpret_cast<uint4*>(dst + lane * 16) = x;
-      return;
-    }
-    float f[8];
+  auto open = [&](const uint4& x, float (&f)[8]) {
     const uint32_t word[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -186,40 +230,58 @@ __global__ void __launch_bounds__(kThreads) ta_cache_append_kernel(ta_cache_move
       f[2 * e] = p.x;
       f[2 * e + 1] = p.y;
     }
-    if (turned) turn(f, w);
-    if constexpr (!CODES) {
-      if (row >= 0)
-        *reinterpret_cast<uint4*>(dst + lane * 16) = make_uint4(pack(f[0], f[1]), pack(f[2], f[3]), pack(f[4], f[5]), pack(f[6], f[7]));
-    } else {
-      // the largest magnitude, as bits: those of infinities and NaN are the largest of all
-      uint32_t top = __float_as_uint(0x1p-100f);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[e]) & 0x7fffffffu);
-#pragma unroll
-      for (int o = N / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-      const bool bad = top >= 0x7f800000u;
-      constexpr float FULL = FMT == TA_CACHE_E4M3 ? 448.0f : 127.0f;
-      const float m = __uint_as_float(top), inv = __fdiv_rn(FULL, m);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = bad ? 0.0f : f[e] * inv;
-      uint2 code;
-      if constexpr (FMT == TA_CACHE_E4M3) code = make_uint2(e4m3x4(f[0], f[1], f[2], f[3]), e4m3x4(f[4], f[5], f[6], f[7]));
-      else code = make_uint2(int8x4(f[0], f[1], f[2], f[3]), int8x4(f[4], f[5], f[6], f[7]));
-      if (row >= 0) {
-        *reinterpret_cast<uint2*>(dst + lane * 8) = code;
-        if (lane == 0) scales[s_place[w].scale] = bad ? __int_as_float(0x7fc00000) : __fdiv_rn(m, FULL);
-      }
-    }
   };
-
+  auto largest = [&](const float (&f)[8]) {  // magnitude in a row; a NaN is larger than all
+    float m = fabsf(f[0]);
+#pragma unroll
+    for (int e = 1; e < 8; ++e) m = max_nan(m, fabsf(f[e]));
+#pragma unroll
+    for (int o = N / 2; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+    return m;
+  };
+  auto code = [&](const float (&f)[8], float inv, bool fine) {
+    uint2 r;
+    if constexpr (FMT == TA_CACHE_E4M3)
+      r = make_uint2(e4m3x4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv), e4m3x4(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv));
+    else r = make_uint2(int8x4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv), int8x4(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv));
+    return fine ? r : make_uint2(0u, 0u);
+  };
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    if (i * GROUPS >= todo) break;  // (the same for all lanes of a warp: shuffles)
-    const bool is = group + i * GROUPS < todo;  // a group without an item goes along and writes nothing
-    const int w = is ? group + i * GROUPS : 0;
+    const int w = group * PER + i;
+    const bool is = w < todo;  // a group without an item goes along (shuffles) and writes nothing
     if (!is) k[i] = v[i] = make_uint4(0u, 0u, 0u, 0u);
-    put(k[i], w, is, TURN, c.k, c.ks);
-    put(v[i], w, is, false, c.v, c.vs);
+    const Place place = s_place[is ? w : 0];
+    const bool put = is && place.row >= 0;
+    float f[8];
+    if constexpr (!CODES) {
+      if constexpr (TURN) {
+        open(k[i], f);
+        turn(f, k[i], is ? w : 0);
+        k[i] = make_uint4(pack(f[0], f[1]), pack(f[2], f[3]), pack(f[4], f[5]), pack(f[6], f[7]));
+      }
+      if (put) {
+        *reinterpret_cast<uint4*>(c.k + place.row + lane * 16) = k[i];
+        *reinterpret_cast<uint4*>(c.v + place.row + lane * 16) = v[i];
+      }
+    } else {
+      float h[8];
+      open(k[i], f);
+      if constexpr (TURN) turn(f, k[i], is ? w : 0);
+      open(v[i], h);
+      const float mk = largest(f), mv = largest(h);
+      // one lane divides for the keys, the next for the values
+      constexpr float FULL = FMT == TA_CACHE_E4M3 ? 448.0f : 127.0f;
+      const float mine = (lane & 1) ? mv : mk, m = fmaxf(mine, 0x1p-100f), quotient = __fdiv_rn(FULL, m);
+      const int leader = (threadIdx.x & 31) - lane;
+      const float ik = __shfl_sync(0xffffffffu, quotient, leader), iv = __shfl_sync(0xffffffffu, quotient, leader + 1);
+      const uint2 ck = code(f, ik, mk < INFINITY), cv = code(h, iv, mv < INFINITY);
+      if (put) {
+        *reinterpret_cast<uint2*>(c.k + place.row + lane * 8) = ck;
+        *reinterpret_cast<uint2*>(c.v + place.row + lane * 8) = cv;
+        if (lane < 2) (lane ? c.vs : c.ks)[place.scale] = mine < INFINITY ? ta_div_by(m, FULL, __frcp_rn(FULL)) : __int_as_float(0x7fc00000);
+      }
+    }
   }
 }
 
@@ -230,6 +292,7 @@ __global__ void __launch_bounds__(kThreads) ta_cache_read_kernel(ta_cache_move_a
   constexpr int N = Lanes<D>::N, GROUPS = Lanes<D>::GROUPS, PER = kItems / GROUPS;
   constexpr bool CODES = FMT != TA_CACHE_BF16;
   __shared__ Place s_place[kItems];
+  __shared__ Sides s_side[kItems];
   __shared__ float2 s_scale[kItems];
   const ta_cache_dev& c = a.cache;
   const int lane = threadIdx.x % N, group = threadIdx.x / N, l = blockIdx.y;
@@ -251,16 +314,13 @@ __global__ void __launch_bounds__(kThreads) ta_cache_read_kernel(ta_cache_move_a
       t.b = (int)(u / (unsigned)c.Hkv);
       g = (int)(u - (unsigned)t.b * c.Hkv);
     }
-    Place p;
-    p.k = view_at(a.k, a.seq, l, g, t, tok);
-    p.v = view_at(a.v, a.seq, l, g, t, tok);
+    s_side[threadIdx.x] = {view_at(a.k, a.seq, l, g, t, tok), view_at(a.v, a.seq, l, g, t, tok)};
     const int row = a.rows ? a.rows[rows_at(a.seq, c.Hkv, l, g, t, tok)] : t.i;
     const ta_row_at at = row >= 0 ? ta_cache_row(c, t.b, row) : ta_row_at{-1, 0};
     if (row >= 0 && at.row < 0 && threadIdx.x < todo) ta_report_bounds(status, 31, t.b, row);
-    p.row = at.row < 0 ? -1 : l * c.sl + g * c.sh + at.row;
-    s_place[threadIdx.x] = p;
+    const long long at_scale = l * c.ssl + g * c.ssh + at.scale;
+    s_place[threadIdx.x] = {at.row < 0 ? -1 : l * c.sl + g * c.sh + at.row, at_scale};
     if constexpr (CODES) {
-      const long long at_scale = l * c.ssl + g * c.ssh + at.scale;
       s_scale[threadIdx.x] = at.row < 0 ? make_float2(0.0f, 0.0f) : make_float2(c.ks[at_scale], c.vs[at_scale]);
     }
   }
@@ -312,7 +372,7 @@ __global__ void __launch_bounds__(kThreads) ta_cache_read_kernel(ta_cache_move_a
       } else {
         o = x[k][kv];
       }
-      uint16_t* dst = reinterpret_cast<uint16_t*>(const_cast<void*>(kv ? a.v.ptr : a.k.ptr)) + (kv ? s_place[w].v : s_place[w].k) + lane * 8;
+      uint16_t* dst = reinterpret_cast<uint16_t*>(const_cast<void*>(kv ? a.v.ptr : a.k.ptr)) + (kv ? s_side[w].v : s_side[w].k) + lane * 8;
       ta_st_stream(reinterpret_cast<uint4*>(dst), o);
     }
   }

@@ -142,7 +142,8 @@ __device__ __forceinline__ void ta_st_stream(uint4* p, uint4 v) {
 
 // x / n rounded to nearest for whole numbers 0 <= x <= 2^24 and 1 <= n <= 2^24, given r = 1/n rounded to nearest: one
 // product and one residual correction, which is correctly rounded because r is (Markstein's theorem; no over- or underflow
-// in this range). Many tokens share n: three instructions a quotient, where a division costs about twenty.
+// in this range). Many tokens share n: three instructions a quotient, where a division costs about twenty. (Also for any x and
+// n whose quotient and residual, 2^-24 of x, are normal numbers.)
 __device__ __forceinline__ float ta_div_by(float x, float n, float r) {
   const float q = __fmul_rn(x, r);
   return __fmaf_rn(__fmaf_rn(-q, n, x), r, q);
