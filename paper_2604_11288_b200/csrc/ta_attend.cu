@@ -214,6 +214,7 @@ __global__ void __launch_bounds__(kThreads, (FMT != TA_CACHE_BF16 && MB < 2) ? 3
   int* s_last = reinterpret_cast<int*>(s_there + kWarps * S::STAGES);
 
   ta_wait_for_prior_grid();
+  ta_launch_dependents();
   const ta_cache_dev& c = a.cache;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3;
   const int group = blockIdx.x / pieces, part = blockIdx.x - group * pieces;
@@ -768,6 +769,7 @@ __global__ void __launch_bounds__(kThreads, (FMT != TA_CACHE_BF16 && MB < 2) ? 3
 // Attention mass per cache row, from the scores and the rows' maxima and sums. grid.x = units, grid.y = stretches of rows.
 __global__ void __launch_bounds__(256) ta_attend_mass_kernel(ta_attend_args a, Scratch sc) {
   ta_wait_for_prior_grid();
+  ta_launch_dependents();
   const int unit = blockIdx.x;
   const Unit u = unit_of(a, unit, false, nullptr);
   const int G = a.Hq / a.cache.Hkv, rows = G * a.T;

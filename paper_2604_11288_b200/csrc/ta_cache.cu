@@ -12,30 +12,44 @@
 namespace {
 
 constexpr int kThreads = 128;
-constexpr int kItems = 32;  // rows of k, and of v, of a block
+// Rows of k, and of v, of a block: 32 keep memory busy (16: 2989 us where 32 take 2722, see below), 8 spread a call with few
+// rows over more SMs.
+constexpr int kItems = 32, kFewItems = 8;
+constexpr long long kFewRows = 148 * 32;
 
 struct Token {
   int b, i;  // sequence and index in it
 };
-// The sequence of a token, looked for by a whole warp: 32 offsets at a time, not one after another.
-__device__ __forceinline__ int sequence_of(const ta_seq_desc& seq, long long tok) {
-  const int lane = threadIdx.x & 31;
-  int b = -1;
-  for (int at = 0; at < seq.batch; at += 32) {  // the last sequence that begins at or before the token
-    const int n = __popc(__ballot_sync(0xffffffffu, at + lane < seq.batch && seq.cu[at + lane] <= tok));
-    b += n;
-    if (n < 32) break;
+// What the tokens of a block are looked up in: the offsets of the sequences and, where every sequence has one, their lengths.
+// Few of them are brought to shared memory, all at once: one wait where a search and a length would be one after another.
+constexpr int kKept = 256;
+struct Kept {
+  int cu[kKept + 1], len[kKept];
+};
+__device__ __forceinline__ bool keeps(const ta_seq_desc& seq) { return seq.batch <= kKept; }
+__device__ __forceinline__ void keep(Kept& s, const ta_seq_desc& seq, const ta_cache_dev& c, bool with_lens) {
+  if (!keeps(seq)) return;
+  for (int i = threadIdx.x; i <= seq.batch; i += kThreads) {
+    if (seq.cu) s.cu[i] = seq.cu[i];
+    if (with_lens && i < seq.batch) s.len[i] = c.lens && !c.lens_per_unit ? c.lens[i] : c.len_uniform;
   }
-  return max(b, 0);
 }
-// Token tok of the batch; b0: the sequence of a token shortly before it.
-__device__ __forceinline__ Token token_of(const ta_seq_desc& seq, long long tok, int b0) {
+__device__ __forceinline__ Token token_of(const Kept& s, const ta_seq_desc& seq, long long tok) {
   if (!seq.cu) {
     const int b = (int)((unsigned)tok / (unsigned)seq.n_uniform);
     return {b, (int)(tok - (long long)b * seq.n_uniform)};
   }
-  while (b0 + 1 < seq.batch && seq.cu[b0 + 1] <= tok) ++b0;
-  return {b0, (int)(tok - seq.cu[b0])};
+  const int* cu = keeps(seq) ? s.cu : seq.cu;
+  int lo = 0, hi = seq.batch;  // the last sequence that begins at or before the token
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (cu[mid] <= tok) lo = mid;
+    else hi = mid;
+  }
+  return {lo, (int)(tok - cu[lo])};
+}
+__device__ __forceinline__ int len_of(const Kept& s, const ta_seq_desc& seq, const ta_cache_dev& c, int l, int b, int g) {
+  return keeps(seq) && !(c.lens && c.lens_per_unit) ? s.len[b] : ta_cache_len(c, l, b, g);
 }
 __device__ __forceinline__ long long view_at(const ta_bf16_view& v, const ta_seq_desc& seq, int l, int g, Token t, long long tok) {
   return l * v.stride_l + g * v.stride_h + (seq.cu ? tok * v.stride_n : t.b * v.stride_b + t.i * v.stride_n);
@@ -93,17 +107,19 @@ struct Lanes {
   static constexpr int N = D / 8, GROUPS = kThreads / N;
 };
 
-// Items are counted token * Hkv + head. grid.x = kItems of them, grid.y = layers.
-template <int D, int FMT, bool TURN>
-__global__ void __launch_bounds__(kThreads) ta_cache_append_kernel(ta_cache_move_args a, ta_dev_status* status) {
+// Items are counted token * Hkv + head. grid.x = ITEMS of them, grid.y = layers.
+template <int D, int FMT, bool TURN, int ITEMS>
+__global__ void __launch_bounds__(kThreads, 8) ta_cache_append_kernel(ta_cache_move_args a, ta_dev_status* status) {
   ta_wait_for_prior_grid();
-  constexpr int N = Lanes<D>::N, GROUPS = Lanes<D>::GROUPS, PER = kItems / GROUPS;
+  ta_launch_dependents();
+  constexpr int N = Lanes<D>::N, GROUPS = Lanes<D>::GROUPS, PER = ITEMS / GROUPS;
   constexpr bool CODES = FMT != TA_CACHE_BF16;
   extern __shared__ float2 s_cs[];  // [token][pair]
-  __shared__ Place s_place[kItems];
+  __shared__ Place s_place[ITEMS];
+  __shared__ Kept s_kept;
   const ta_cache_dev& c = a.cache;
   const int lane = threadIdx.x % N, group = threadIdx.x / N, l = blockIdx.y, half = a.rot.d_rot / 2;
-  const unsigned first = blockIdx.x * kItems, todo = min((unsigned)kItems, (unsigned)a.seq.total * c.Hkv - first);
+  const unsigned first = blockIdx.x * ITEMS, todo = min((unsigned)ITEMS, (unsigned)a.seq.total * c.Hkv - first);
   const unsigned tok0 = first / c.Hkv, tokens = (first + todo - 1) / c.Hkv - tok0 + 1;
   // a group of lanes has PER items that follow one another: heads of one token, as a rule
   uint4 k[PER], v[PER];
@@ -116,7 +132,7 @@ __global__ void __launch_bounds__(kThreads) ta_cache_append_kernel(ta_cache_move
     for (int i = 0; i < PER; ++i) {
       if (i == 0 || g == 0) {  // a token's first item here
         Token t = {0, 0};
-        if (!a.seq.cu) t = token_of(a.seq, tok, 0);
+        if (!a.seq.cu) t = token_of(s_kept, a.seq, tok);
         kp = reinterpret_cast<const __nv_bfloat16*>(a.k.ptr) + view_at(a.k, a.seq, l, g, t, tok) + lane * 8;
         vp = reinterpret_cast<const __nv_bfloat16*>(a.v.ptr) + view_at(a.v, a.seq, l, g, t, tok) + lane * 8;
       }
@@ -129,14 +145,15 @@ __global__ void __launch_bounds__(kThreads) ta_cache_append_kernel(ta_cache_move
       if (++g == c.Hkv) g = 0, ++tok;
     }
   }
-  const int b0 = a.seq.cu ? sequence_of(a.seq, tok0) : 0;
+  keep(s_kept, a.seq, c, !a.rows || TURN);
+  __syncthreads();
   // one thread finds an item's place, while the others form the angles
   if (threadIdx.x < todo) {
     const unsigned w = first + threadIdx.x, tok = w / c.Hkv;
     const int g = (int)(w - tok * c.Hkv);
-    const Token t = token_of(a.seq, tok, b0);
+    const Token t = token_of(s_kept, a.seq, tok);
     Place p;
-    const long long row = a.rows ? (long long)a.rows[rows_at(a.seq, c.Hkv, l, g, t, tok)] : (long long)ta_cache_len(c, l, t.b, g) + t.i;
+    const long long row = a.rows ? (long long)a.rows[rows_at(a.seq, c.Hkv, l, g, t, tok)] : (long long)len_of(s_kept, a.seq, c, l, t.b, g) + t.i;
     ta_row_at at = {-1, 0};
     if (row >= 0 && row < 0x7fffffff) at = ta_cache_row(c, t.b, (int)row);
     if (at.row < 0 && (row >= 0 || !a.rows)) ta_report_bounds(status, 30, t.b, (int)row);
@@ -151,8 +168,8 @@ __global__ void __launch_bounds__(kThreads) ta_cache_append_kernel(ta_cache_move
       if (a.rot.positions) {
         position = a.rot.positions[tok];
       } else {
-        const Token t = token_of(a.seq, tok, b0);  // the row, the same for all layers and heads
-        position = ta_cache_len(c, l, t.b, 0) + t.i;
+        const Token t = token_of(s_kept, a.seq, tok);  // the row, the same for all layers and heads
+        position = len_of(s_kept, a.seq, c, l, t.b, 0) + t.i;
       }
       s_cs[w] = ta_cos_sin(a.rot, a.rot.phase[p], position);
     }
@@ -285,29 +302,33 @@ __global__ void __launch_bounds__(kThreads) ta_cache_append_kernel(ta_cache_move
   }
 }
 
-// Items in the order [B][Hkv][n], or [Hkv][total] where the batch is ragged. grid.x = kItems of them, grid.y = layers.
-template <int D, int FMT>
+// Items in the order [B][Hkv][n], or [Hkv][total] where the batch is ragged. grid.x = ITEMS of them, grid.y = layers.
+template <int D, int FMT, int ITEMS>
 __global__ void __launch_bounds__(kThreads) ta_cache_read_kernel(ta_cache_move_args a, ta_dev_status* status) {
   ta_wait_for_prior_grid();
-  constexpr int N = Lanes<D>::N, GROUPS = Lanes<D>::GROUPS, PER = kItems / GROUPS;
+  ta_launch_dependents();
+  constexpr int N = Lanes<D>::N, GROUPS = Lanes<D>::GROUPS, PER = ITEMS / GROUPS;
   constexpr bool CODES = FMT != TA_CACHE_BF16;
-  __shared__ Place s_place[kItems];
-  __shared__ Sides s_side[kItems];
-  __shared__ float2 s_scale[kItems];
+  __shared__ Place s_place[ITEMS];
+  __shared__ Kept s_kept;
+  __shared__ Sides s_side[ITEMS];
+  __shared__ float2 s_scale[ITEMS];
   const ta_cache_dev& c = a.cache;
   const int lane = threadIdx.x % N, group = threadIdx.x / N, l = blockIdx.y;
-  const unsigned first = blockIdx.x * kItems, todo = min((unsigned)kItems, (unsigned)a.seq.total * c.Hkv - first);
-  if (threadIdx.x < 32) {  // a lane finds an item's places
-    const unsigned w = first + min(threadIdx.x, todo - 1);
+  const unsigned first = blockIdx.x * ITEMS, todo = min((unsigned)ITEMS, (unsigned)a.seq.total * c.Hkv - first);
+  if (a.seq.cu) {
+    keep(s_kept, a.seq, c, false);
+    __syncthreads();
+  }
+  if (threadIdx.x < todo) {  // one thread finds an item's places
+    const unsigned w = first + threadIdx.x;
     Token t;
     int g;
     unsigned tok = 0;
     if (a.seq.cu) {
       g = (int)(w / (unsigned)a.seq.total);
       tok = w - (unsigned)g * (unsigned)a.seq.total;
-      const unsigned tok0 = __shfl_sync(0xffffffffu, tok, 0);
-      const int b0 = sequence_of(a.seq, tok0);
-      t = token_of(a.seq, tok, tok >= tok0 ? b0 : 0);  // (the next head's tokens begin anew)
+      t = token_of(s_kept, a.seq, tok);
     } else {
       const unsigned u = w / (unsigned)a.seq.n_uniform;
       t.i = (int)(w - u * a.seq.n_uniform);
@@ -317,7 +338,7 @@ __global__ void __launch_bounds__(kThreads) ta_cache_read_kernel(ta_cache_move_a
     s_side[threadIdx.x] = {view_at(a.k, a.seq, l, g, t, tok), view_at(a.v, a.seq, l, g, t, tok)};
     const int row = a.rows ? a.rows[rows_at(a.seq, c.Hkv, l, g, t, tok)] : t.i;
     const ta_row_at at = row >= 0 ? ta_cache_row(c, t.b, row) : ta_row_at{-1, 0};
-    if (row >= 0 && at.row < 0 && threadIdx.x < todo) ta_report_bounds(status, 31, t.b, row);
+    if (row >= 0 && at.row < 0) ta_report_bounds(status, 31, t.b, row);
     const long long at_scale = l * c.ssl + g * c.ssh + at.scale;
     s_place[threadIdx.x] = {at.row < 0 ? -1 : l * c.sl + g * c.sh + at.row, at_scale};
     if constexpr (CODES) {
@@ -378,9 +399,9 @@ __global__ void __launch_bounds__(kThreads) ta_cache_read_kernel(ta_cache_move_a
   }
 }
 
-cudaLaunchConfig_t config(const ta_cache_move_args& a, cudaStream_t stream, cudaLaunchAttribute* attr) {
+cudaLaunchConfig_t config(const ta_cache_move_args& a, int items, cudaStream_t stream, cudaLaunchAttribute* attr) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((a.seq.total * a.cache.Hkv + kItems - 1) / kItems), (unsigned)a.n_layers, 1);
+  cfg.gridDim = dim3((unsigned)((a.seq.total * a.cache.Hkv + items - 1) / items), (unsigned)a.n_layers, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
   cfg.stream = stream;
   ta_pdl_attribute(attr);
@@ -388,43 +409,43 @@ cudaLaunchConfig_t config(const ta_cache_move_args& a, cudaStream_t stream, cuda
   cfg.numAttrs = 1;
   return cfg;
 }
-template <int D, int FMT>
+template <int D, int FMT, int ITEMS>
 cudaError_t append(const ta_cache_move_args& a, ta_dev_status* status, cudaStream_t stream) {
   cudaLaunchAttribute attr[1];
-  cudaLaunchConfig_t cfg = config(a, stream, attr);
-  if (!a.rot.phase) return cudaLaunchKernelEx(&cfg, ta_cache_append_kernel<D, FMT, false>, a, status);
-  const int tokens = (kItems + a.cache.Hkv - 2) / a.cache.Hkv + 1;  // that a block's items may belong to
+  cudaLaunchConfig_t cfg = config(a, ITEMS, stream, attr);
+  if (!a.rot.phase) return cudaLaunchKernelEx(&cfg, ta_cache_append_kernel<D, FMT, false, ITEMS>, a, status);
+  const int tokens = (ITEMS + a.cache.Hkv - 2) / a.cache.Hkv + 1;  // that a block's items may belong to
   cfg.dynamicSmemBytes = (size_t)tokens * (a.rot.d_rot / 2) * sizeof(float2);
-  return cudaLaunchKernelEx(&cfg, ta_cache_append_kernel<D, FMT, true>, a, status);
+  return cudaLaunchKernelEx(&cfg, ta_cache_append_kernel<D, FMT, true, ITEMS>, a, status);
 }
-template <int D, int FMT>
+template <int D, int FMT, int ITEMS>
 cudaError_t read(const ta_cache_move_args& a, ta_dev_status* status, cudaStream_t stream) {
   cudaLaunchAttribute attr[1];
-  cudaLaunchConfig_t cfg = config(a, stream, attr);
-  return cudaLaunchKernelEx(&cfg, ta_cache_read_kernel<D, FMT>, a, status);
+  cudaLaunchConfig_t cfg = config(a, ITEMS, stream, attr);
+  return cudaLaunchKernelEx(&cfg, ta_cache_read_kernel<D, FMT, ITEMS>, a, status);
+}
+template <int D, int FMT>
+cudaError_t move(bool write, const ta_cache_move_args& a, ta_dev_status* status, cudaStream_t stream) {
+  // (a block has 128 / (D / 8) groups of lanes and at least one row for each)
+  constexpr int FEW = kFewItems > Lanes<D>::GROUPS ? kFewItems : Lanes<D>::GROUPS;
+  if (a.seq.total * a.cache.Hkv * a.n_layers <= kFewRows)
+    return write ? append<D, FMT, FEW>(a, status, stream) : read<D, FMT, FEW>(a, status, stream);
+  return write ? append<D, FMT, kItems>(a, status, stream) : read<D, FMT, kItems>(a, status, stream);
+}
+template <int D>
+cudaError_t move(bool write, const ta_cache_move_args& a, ta_dev_status* status, cudaStream_t stream) {
+  if (a.cache.format == TA_CACHE_BF16) return move<D, TA_CACHE_BF16>(write, a, status, stream);
+  if (a.cache.format == TA_CACHE_E4M3) return move<D, TA_CACHE_E4M3>(write, a, status, stream);
+  return move<D, TA_CACHE_INT8>(write, a, status, stream);
 }
 
 }  // namespace
 
 cudaError_t ta_launch_cache_append(const ta_cache_move_args& a, ta_dev_status* status, cudaStream_t stream) {
   if (a.seq.total == 0) return cudaSuccess;
-  const int f = a.cache.format;
-  if (a.d == 64)
-    return f == TA_CACHE_BF16 ? append<64, TA_CACHE_BF16>(a, status, stream)
-           : f == TA_CACHE_E4M3 ? append<64, TA_CACHE_E4M3>(a, status, stream)
-                                : append<64, TA_CACHE_INT8>(a, status, stream);
-  return f == TA_CACHE_BF16 ? append<128, TA_CACHE_BF16>(a, status, stream)
-         : f == TA_CACHE_E4M3 ? append<128, TA_CACHE_E4M3>(a, status, stream)
-                              : append<128, TA_CACHE_INT8>(a, status, stream);
+  return a.d == 64 ? move<64>(true, a, status, stream) : move<128>(true, a, status, stream);
 }
 cudaError_t ta_launch_cache_read(const ta_cache_move_args& a, ta_dev_status* status, cudaStream_t stream) {
   if (a.seq.total == 0) return cudaSuccess;
-  const int f = a.cache.format;
-  if (a.d == 64)
-    return f == TA_CACHE_BF16 ? read<64, TA_CACHE_BF16>(a, status, stream)
-           : f == TA_CACHE_E4M3 ? read<64, TA_CACHE_E4M3>(a, status, stream)
-                                : read<64, TA_CACHE_INT8>(a, status, stream);
-  return f == TA_CACHE_BF16 ? read<128, TA_CACHE_BF16>(a, status, stream)
-         : f == TA_CACHE_E4M3 ? read<128, TA_CACHE_E4M3>(a, status, stream)
-                              : read<128, TA_CACHE_INT8>(a, status, stream);
+  return a.d == 64 ? move<64>(false, a, status, stream) : move<128>(false, a, status, stream);
 }
