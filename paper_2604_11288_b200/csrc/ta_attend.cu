@@ -40,7 +40,7 @@ struct Shape {
   static constexpr int TK = (CODES || D == 64) ? 32 : 16;         // cache rows of a tile
   static constexpr int TILE = TK * ROW;                           // bytes of K, and of V, in a stage
   static constexpr int STAGE = 2 * TILE + (CODES ? 2 * TK * 4 : 0);
-  static constexpr int STAGES = CODES ? 2 : 3;
+  static constexpr int STAGES = 2;
   static constexpr int KS = D / 16;                               // products along d
   static constexpr int RING = kWarps * STAGES * STAGE;
 };
@@ -51,7 +51,7 @@ constexpr int smem_bytes() {
   constexpr int q32 = R * D * 4;  // queries in fp32, then (MB > 0) their fragments, hi and lo, in the same place
   constexpr int join = kWarps * R * (D + 4) * 4;
   constexpr int ring = Shape<D, FMT>::RING > join ? Shape<D, FMT>::RING : join;
-  return ring + q32 + R * 8 /* row factor, limit */ + kWarps * R * 8 /* m, l */ + kWarps * Shape<D, FMT>::STAGES * 4 + 16;
+  return ring + q32 + R * 4 /* row factors */ + kWarps * R * 8 /* maxima and sums */ + kWarps * Shape<D, FMT>::STAGES * 4 + 16;
 }
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool there) {
@@ -195,7 +195,7 @@ __device__ __forceinline__ float joined_max(const float2* ml, int parts, long lo
 
 // blockIdx.x = (unit * row blocks + block) * pieces + piece
 template <int D, int FMT, int MB>
-__global__ void __launch_bounds__(kThreads, (FMT != TA_CACHE_BF16 && MB < 2) ? 3 : 2) ta_attend_kernel(ta_attend_args a, Scratch sc, int pieces, int piece, int row_blocks,
+__global__ void __launch_bounds__(kThreads, MB < 2 ? 3 : 2) ta_attend_kernel(ta_attend_args a, Scratch sc, int pieces, int piece, int row_blocks,
                                                               uint32_t times128, ta_dev_status* status) {
   using S = Shape<D, FMT>;
   constexpr bool CODES = S::CODES, NARROW = MB == 0;
@@ -208,8 +208,7 @@ __global__ void __launch_bounds__(kThreads, (FMT != TA_CACHE_BF16 && MB < 2) ? 3
   uint4* s_frag = reinterpret_cast<uint4*>(s_at);  // [hi, lo][mb][ks][lane]
   s_at += R * D * 4;
   float* s_factor = reinterpret_cast<float*>(s_at);
-  int* s_limit = reinterpret_cast<int*>(s_factor + R);
-  float2* s_ml = reinterpret_cast<float2*>(s_limit + R);
+  float2* s_ml = reinterpret_cast<float2*>(s_factor + R);
   uint32_t* s_there = reinterpret_cast<uint32_t*>(s_ml + kWarps * R);
   int* s_last = reinterpret_cast<int*>(s_there + kWarps * S::STAGES);
 
@@ -278,44 +277,46 @@ __global__ void __launch_bounds__(kThreads, (FMT != TA_CACHE_BF16 && MB < 2) ? 3
 #pragma unroll
   for (int i = 0; i < S::STAGES - 1; ++i) issue(i);
 
-  // ---- the queries: fp32 in shared memory, rotated, then fragments
-  for (int w = tid; w < R * D; w += kThreads) {
-    const int r = w / D, j = w - r * D, row = r0 + r;
-    float v = 0.0f;
-    if (row < rows) {
-      const int t = row / G, h = u.g * G + row - t * G;
-      const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(a.q.ptr) + u.l * a.q.stride_l + u.b * a.q.stride_b +
-                               h * a.q.stride_h + t * a.q.stride_n;
-      v = __bfloat162float(q[j]);
-      if (a.rot.phase && j < a.rot.d_rot) {
-        const int half = a.rot.d_rot / 2;
-        const int position = a.rot.positions ? a.rot.positions[u.b * a.T + t] : u.n - a.T + t;
-        const bool second = a.rot.interleaved ? (j & 1) : j >= half;
-        const int p = a.rot.interleaved ? j >> 1 : (second ? j - half : j);
-        const int other = a.rot.interleaved ? j ^ 1 : (second ? j - half : j + half);
-        const float2 cs = ta_cos_sin(a.rot, a.rot.phase[p], position);
-        const float o = __bfloat162float(q[other]);
-        v = second ? o * cs.y + v * cs.x : v * cs.x - o * cs.y;
+  // ---- the queries
+  auto limit_of = [&](int r) {  // cache rows that the block's row r sees
+    const int row = r0 + r;
+    return row < rows ? max(0, u.n - (a.causal ? a.T - 1 - row / G : 0)) : 0;
+  };
+  auto query = [&](int row) {
+    const int t = row / G, h = u.g * G + row - t * G;
+    return reinterpret_cast<const __nv_bfloat16*>(a.q.ptr) + u.l * a.q.stride_l + u.b * a.q.stride_b + h * a.q.stride_h +
+           t * a.q.stride_n;
+  };
+  // up to 8 rows that are not rotated go straight to the fragments, others to shared memory in fp32 first
+  const bool straight = NARROW && !a.rot.phase;
+  if (!straight) {
+    for (int w = tid; w < R * D; w += kThreads) {
+      const int r = w / D, j = w - r * D, row = r0 + r;
+      float v = 0.0f;
+      if (row < rows) {
+        const __nv_bfloat16* q = query(row);
+        v = __bfloat162float(q[j]);
+        if (a.rot.phase && j < a.rot.d_rot) {
+          const int half = a.rot.d_rot / 2;
+          const int position = a.rot.positions ? a.rot.positions[u.b * a.T + row / G] : u.n - a.T + row / G;
+          const bool second = a.rot.interleaved ? (j & 1) : j >= half;
+          const int p = a.rot.interleaved ? j >> 1 : (second ? j - half : j);
+          const int other = a.rot.interleaved ? j ^ 1 : (second ? j - half : j + half);
+          const float2 cs = ta_cos_sin(a.rot, a.rot.phase[p], position);
+          const float o = __bfloat162float(q[other]);
+          v = second ? o * cs.y + v * cs.x : v * cs.x - o * cs.y;
+        }
       }
+      s_q[w] = v;
     }
-    s_q[w] = v;
+    __syncthreads();
   }
-  if (tid < R) {
-    const int row = r0 + tid;
-    s_limit[tid] = row < rows ? max(0, u.n - (a.causal ? a.T - 1 - row / G : 0)) : 0;
-  }
-  __syncthreads();
   // a row's part of four coordinates for product ks: the order in which a lane's bytes of a key row come
   auto coordinate = [&](int ks) { return CODES ? (t4 + 4 * (ks / 4)) * 16 + (ks % 4) * 4 : (t4 + 4 * (ks / 2)) * 8 + (ks % 2) * 4; };
   const float bits = a.scale * 1.4426950408889634f * pow2(kCodeUnit<FMT>);
-  auto row_scale = [&](int r, float& down) {  // 8-bit caches: a power of two that brings the row's largest value into [1, 2)
-    float m = 0.0f;
+  // 8-bit caches: a power of two that brings a row's largest value into [1, 2); m: the largest of this lane's
+  auto row_scale = [&](float m, float& down) {
     if constexpr (CODES) {
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const float4 v = *reinterpret_cast<const float4*>(s_q + r * D + coordinate(ks));
-        m = fmaxf(m, fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w))));
-      }
       m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
       m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
     }
@@ -323,20 +324,61 @@ __global__ void __launch_bounds__(kThreads, (FMT != TA_CACHE_BF16 && MB < 2) ? 3
     down = pow2(-e);
     return bits * pow2(e);
   };
+  auto largest = [](float m, const float4& v) { return fmaxf(m, fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w)))); };
+  auto staged = [&](int r, int at) { return *reinterpret_cast<const float4*>(s_q + r * D + at); };
+  auto staged_scale = [&](int r, float& down) {
+    float m = 0.0f;
+    if constexpr (CODES) {
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) m = largest(m, staged(r, coordinate(ks)));
+    }
+    return row_scale(m, down);
+  };
   uint32_t qf[NARROW ? KS : 1][4];
   float factor[NR];
   int limit[NR];
   if constexpr (NARROW) {
     float down;
-    factor[0] = row_scale(g8, down);
-    limit[0] = s_limit[g8];
+    limit[0] = limit_of(g8);
+    if (straight) {
+      const bool is = r0 + g8 < rows;
+      const __nv_bfloat16* q = is ? query(r0 + g8) : nullptr;
+      uint2 w[KS];
+      float m = 0.0f;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const float4 v = *reinterpret_cast<const float4*>(s_q + g8 * D + coordinate(ks));
-      qf[ks][0] = pack2<CODES>(v.x * down, v.y * down);
-      qf[ks][2] = pack2<CODES>(v.z * down, v.w * down);
-      qf[ks][1] = rest2<CODES>(v.x * down, v.y * down, qf[ks][0]);
-      qf[ks][3] = rest2<CODES>(v.z * down, v.w * down, qf[ks][2]);
+      for (int ks = 0; ks < KS; ++ks) w[ks] = is ? *reinterpret_cast<const uint2*>(q + coordinate(ks)) : make_uint2(0u, 0u);
+      if constexpr (CODES) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const float2 x = unpack2<false>(w[ks].x), y = unpack2<false>(w[ks].y);
+          m = largest(m, make_float4(x.x, x.y, y.x, y.y));
+        }
+      }
+      factor[0] = row_scale(m, down);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        if constexpr (CODES) {
+          const float2 x = unpack2<false>(w[ks].x), y = unpack2<false>(w[ks].y);
+          qf[ks][0] = pack2<CODES>(x.x * down, x.y * down);
+          qf[ks][2] = pack2<CODES>(y.x * down, y.y * down);
+          qf[ks][1] = rest2<CODES>(x.x * down, x.y * down, qf[ks][0]);
+          qf[ks][3] = rest2<CODES>(y.x * down, y.y * down, qf[ks][2]);
+        } else {
+          qf[ks][0] = w[ks].x;
+          qf[ks][2] = w[ks].y;
+          qf[ks][1] = qf[ks][3] = 0u;
+        }
+      }
+    } else {
+      factor[0] = staged_scale(g8, down);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const float4 v = staged(g8, coordinate(ks));
+        qf[ks][0] = pack2<CODES>(v.x * down, v.y * down);
+        qf[ks][2] = pack2<CODES>(v.z * down, v.w * down);
+        qf[ks][1] = rest2<CODES>(v.x * down, v.y * down, qf[ks][0]);
+        qf[ks][3] = rest2<CODES>(v.z * down, v.w * down, qf[ks][2]);
+      }
     }
   } else {
     constexpr int PER_WARP = KS / kWarps;  // products of a warp, of every 16 rows
@@ -344,13 +386,12 @@ __global__ void __launch_bounds__(kThreads, (FMT != TA_CACHE_BF16 && MB < 2) ? 3
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
       float d0, d1;
-      const float f0 = row_scale(mb * 16 + g8, d0), f1 = row_scale(mb * 16 + g8 + 8, d1);
+      const float f0 = staged_scale(mb * 16 + g8, d0), f1 = staged_scale(mb * 16 + g8 + 8, d1);
       if (warp == 0 && t4 == 0) s_factor[mb * 16 + g8] = f0, s_factor[mb * 16 + g8 + 8] = f1;
 #pragma unroll
       for (int i = 0; i < PER_WARP; ++i) {
         const int at = coordinate(warp * PER_WARP + i);
-        const float4 v = *reinterpret_cast<const float4*>(s_q + (mb * 16 + g8) * D + at);
-        const float4 w = *reinterpret_cast<const float4*>(s_q + (mb * 16 + g8 + 8) * D + at);
+        const float4 v = staged(mb * 16 + g8, at), w = staged(mb * 16 + g8 + 8, at);
         uint4 &h = hi[mb][i], &r = lo[mb][i];
         h.x = pack2<CODES>(v.x * d0, v.y * d0);
         h.y = pack2<CODES>(w.x * d1, w.y * d1);
@@ -374,12 +415,12 @@ __global__ void __launch_bounds__(kThreads, (FMT != TA_CACHE_BF16 && MB < 2) ? 3
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
       factor[i] = s_factor[(i / 2) * 16 + (i & 1) * 8 + g8];
-      limit[i] = s_limit[(i / 2) * 16 + (i & 1) * 8 + g8];
+      limit[i] = limit_of((i / 2) * 16 + (i & 1) * 8 + g8);
     }
   }
   const bool q_parts = a.rot.phase != nullptr;  // queries that are not rotated have no second part
   const uint32_t frag = smem_u32(s_frag) + lane * 16;
-  const int seen_by_all = s_limit[0];  // the block's first row has the lowest limit
+  const int seen_by_all = limit_of(0);  // the block's first row has the lowest limit
 
   float o[MBN][NJ][4], m[NR], l[NR];
 #pragma unroll
@@ -607,7 +648,7 @@ __global__ void __launch_bounds__(kThreads, (FMT != TA_CACHE_BF16 && MB < 2) ? 3
         }
         int before = -1;
         for (int r = 0; r < R; ++r) {  // one product per limit; a row takes the result of its own
-          const int lim = s_limit[r];
+          const int lim = limit_of(r);
           if (lim == before) continue;
           before = lim;
           auto cut = [&](uint32_t v, int k) {
@@ -676,6 +717,7 @@ __global__ void __launch_bounds__(kThreads, (FMT != TA_CACHE_BF16 && MB < 2) ? 3
     l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
     const int row = NARROW ? g8 : (r / 2) * 16 + (r & 1) * 8 + g8;
     if (t4 == 0) s_ml[warp * R + row] = make_float2(m[r], l[r]);
+    if (r0 + row >= rows) continue;
     float* to = s_o + (warp * R + row) * LD;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
@@ -766,22 +808,34 @@ __global__ void __launch_bounds__(kThreads, (FMT != TA_CACHE_BF16 && MB < 2) ? 3
   }
 }
 
-// Attention mass per cache row, from the scores and the rows' maxima and sums. grid.x = units, grid.y = stretches of rows.
+// Attention mass per cache row, from the scores and the rows' maxima and sums; a thread has four cache rows. grid.x = units,
+// grid.y = stretches of 1024 rows. (Formed at the end of the attention's own blocks, where a unit is one block, it took longer:
+// 32 x 16 x 8 units of 257 rows 135 us a step where this takes 128, of 1025 rows 423 and 388.)
 __global__ void __launch_bounds__(256) ta_attend_mass_kernel(ta_attend_args a, Scratch sc) {
   ta_wait_for_prior_grid();
   ta_launch_dependents();
-  const int unit = blockIdx.x;
-  const Unit u = unit_of(a, unit, false, nullptr);
-  const int G = a.Hq / a.cache.Hkv, rows = G * a.T;
-  for (long long j = (long long)blockIdx.y * 256 + threadIdx.x; j < a.mass_stride; j += (long long)gridDim.y * 256) {
-    float sum = 0.0f;
-    for (int r = 0; r < rows; ++r) {
-      if (j >= u.n - (a.causal ? a.T - 1 - r / G : 0)) continue;
-      const float2 ml = sc.row_ml[(long long)unit * rows + r];
-      if (ml.y == 0.0f) continue;  // a token that sees nothing
-      sum += ex2(sc.score[((long long)unit * rows + r) * sc.score_stride + j] - ml.x) * ml.y;
+  const int unit = blockIdx.x, G = a.Hq / a.cache.Hkv, rows = G * a.T;
+  const int n = unit_of(a, unit, false, nullptr).n;
+  const float2* row_ml = sc.row_ml + (long long)unit * rows;
+  const float* score = sc.score + (long long)unit * rows * sc.score_stride;
+  for (long long j = 4LL * (blockIdx.y * 256 + threadIdx.x); j < a.mass_stride; j += 1024LL * gridDim.y) {
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (j < n) {
+#pragma unroll 4
+      for (int r = 0; r < rows; ++r) {
+        const float2 ml = row_ml[r];
+        const float4 x = *reinterpret_cast<const float4*>(score + r * sc.score_stride + j);
+        const int seen = n - (a.causal ? a.T - 1 - r / G : 0);
+        if (ml.y == 0.0f) continue;  // a token that sees nothing
+        if (j < seen) sum[0] += ex2(x.x - ml.x) * ml.y;
+        if (j + 1 < seen) sum[1] += ex2(x.y - ml.x) * ml.y;
+        if (j + 2 < seen) sum[2] += ex2(x.z - ml.x) * ml.y;
+        if (j + 3 < seen) sum[3] += ex2(x.w - ml.x) * ml.y;
+      }
     }
-    a.mass[unit * a.mass_stride + j] = sum;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (j + e < a.mass_stride) a.mass[unit * a.mass_stride + j + e] = sum[e];
   }
 }
 
@@ -800,7 +854,7 @@ Plan plan_of(long long units, int rows, int max_len, bool codes) {
   Plan p;
   p.mb = rows <= 8 ? 0 : rows <= 16 ? 1 : 2;
   p.row_blocks = (rows + rows_of(p.mb) - 1) / rows_of(p.mb);
-  const long long groups = units * p.row_blocks, slots = 148 * (codes && p.mb < 2 ? 3 : 2);
+  const long long groups = units * p.row_blocks, slots = 148 * (p.mb < 2 ? 3 : 2);
   const int most = groups > kAttendTickets ? 1 : max_len <= kPieceUnit ? 1 : (max_len + kPieceUnit - 1) / kPieceUnit;
   int k = 1;
   for (; k < most; ++k) {
@@ -889,7 +943,7 @@ cudaError_t ta_launch_attend(const ta_attend_args& a, int* tickets, ta_dev_statu
   cfg.numAttrs = 1;
   cudaError_t e = a.d == 64 ? launch<64>(a, sc, p, cfg, status) : launch<128>(a, sc, p, cfg, status);
   if (e != cudaSuccess || !a.mass) return e;
-  cfg.gridDim = dim3((unsigned)units, (unsigned)((a.mass_stride + 255) / 256), 1);
+  cfg.gridDim = dim3((unsigned)units, (unsigned)((a.mass_stride + 1023) / 1024), 1);
   cfg.blockDim = dim3(256, 1, 1);
   cfg.dynamicSmemBytes = 0;
   return cudaLaunchKernelEx(&cfg, ta_attend_mass_kernel, a, sc);
