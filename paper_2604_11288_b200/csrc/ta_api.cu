@@ -1165,6 +1165,10 @@ ta_cache_move_args move_args(const ta_cache& cache, const ta_batch& batch, const
   a.rows = rows;
   return a;
 }
+size_t attend_scratch(const ta_cache& c, int Hq, int T, int max_len, bool with_mass) {
+  return ta_attend_scratch(c.n_layers * c.batch * c.Hkv, Hq / c.Hkv * T, c.d, max_len, c.format != TA_CACHE_BF16,
+                           c.lens && !c.lens_per_unit ? c.batch : 0, with_mass);
+}
 ta_status check_attend(const ta_cache* c, int Hq, int T, int max_len) {
   ta_status s = check_cache(c);
   if (s != TA_OK) return s;
@@ -1260,9 +1264,7 @@ ta_status ta_attend_scratch_bytes(const ta_cache* cache, int Hq, int T, int max_
   if (!out_bytes) return TA_ERR_INVALID_ARG;
   ta_status s = check_attend(cache, Hq, T, max_len);
   if (s != TA_OK) return s;
-  *out_bytes = align_up(ta_attend_scratch(cache->n_layers * cache->batch * cache->Hkv, Hq / cache->Hkv * T, cache->d, max_len,
-                                          cache->format != TA_CACHE_BF16, with_mass != 0)) +
-               kAlign;
+  *out_bytes = align_up(attend_scratch(*cache, Hq, T, max_len, with_mass != 0)) + kAlign;
   return TA_OK;
 }
 
@@ -1277,9 +1279,7 @@ ta_status ta_attend(ta_ctx* ctx, const ta_cache* cache, int Hq, int T, int new_r
   if (s == TA_OK) s = check_view(out, true, cache->d);
   if (s != TA_OK) return s;
   if (new_rows < 0 || !(scale >= 0.0f) || !isfinite(scale) || (mass && mass_stride < max_len)) return TA_ERR_INVALID_ARG;
-  const int units = cache->n_layers * cache->batch * cache->Hkv;
-  if (ta_attend_scratch(units, Hq / cache->Hkv * T, cache->d, max_len, cache->format != TA_CACHE_BF16, mass != nullptr) >
-      ctx->scratch_bytes)
+  if (attend_scratch(*cache, Hq, T, max_len, mass != nullptr) > ctx->scratch_bytes)
     return TA_ERR_SCRATCH_TOO_SMALL;
   DeviceGuard guard(ctx->device);
   ctx->cached_epoch = 0;

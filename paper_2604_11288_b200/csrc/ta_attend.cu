@@ -178,6 +178,12 @@ __device__ __forceinline__ Unit unit_of(const ta_attend_args& a, int unit, bool 
   return u;
 }
 
+constexpr int kPieceUnit = 128;  // cache rows: whole rounds of every variant's four warps
+struct Cut {                     // how the kernel's blocks share the cache rows of a unit's row block
+  int pieces, piece, row_blocks;
+  int target;               // 0, or: pieces are as long as gives this many in the whole call; `piece` is not used then
+  int groups_per_sequence;  // units and row blocks of a sequence, for that
+};
 struct Scratch {    // of one call (null: not used)
   float* part;      // [unit][row block][piece][row][D], unnormalised
   float2* part_ml;  // [unit][row block][piece][row]: maximum (in bits) and sum
@@ -195,7 +201,7 @@ __device__ __forceinline__ float joined_max(const float2* ml, int parts, long lo
 
 // blockIdx.x = (unit * row blocks + block) * pieces + piece
 template <int D, int FMT, int MB>
-__global__ void __launch_bounds__(kThreads, MB < 2 ? 3 : 2) ta_attend_kernel(ta_attend_args a, Scratch sc, int pieces, int piece, int row_blocks,
+__global__ void __launch_bounds__(kThreads, MB < 2 ? 3 : 2) ta_attend_kernel(ta_attend_args a, Scratch sc, Cut cut,
                                                               uint32_t times128, ta_dev_status* status) {
   using S = Shape<D, FMT>;
   constexpr bool CODES = S::CODES, NARROW = MB == 0;
@@ -216,10 +222,26 @@ __global__ void __launch_bounds__(kThreads, MB < 2 ? 3 : 2) ta_attend_kernel(ta_
   ta_launch_dependents();
   const ta_cache_dev& c = a.cache;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3;
-  const int group = blockIdx.x / pieces, part = blockIdx.x - group * pieces;
-  const int unit = group / row_blocks, r0 = (group - unit * row_blocks) * R;
+  const int group = blockIdx.x / cut.pieces, part = blockIdx.x - group * cut.pieces;
+  const int unit = group / cut.row_blocks, r0 = (group - unit * cut.row_blocks) * R;
   const Unit u = unit_of(a, unit, part == 0 && r0 == 0 && tid == 0, status);
   const int G = a.Hq / c.Hkv, rows = G * a.T;
+  int piece = cut.piece;
+  if (cut.target) {  // pieces of all sequences' rows shared out evenly, not of max_len
+    const int most = (int)min((long long)a.max_len, (long long)c.wide * c.page);
+    int sum = 0;
+    for (int b = tid; b < c.batch; b += kThreads) sum += (int)max(0LL, min((long long)c.lens[b] + a.new_rows, (long long)most));
+    sum = __reduce_add_sync(0xffffffffu, sum);
+    if (lane == 0) s_there[warp] = (uint32_t)sum;
+    __syncthreads();
+    long long all = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) all += s_there[w];
+    __syncthreads();  // (the words are used again)
+    all *= cut.groups_per_sequence;
+    const int even = (int)((all + cut.target - 1) / cut.target), least = (most + cut.pieces - 1) / cut.pieces;
+    piece = (max(max(even, least), 1) + kPieceUnit - 1) / kPieceUnit * kPieceUnit;
+  }
   const int n_pieces = max(1, (u.n + piece - 1) / piece);  // at least one, which writes the empty result
   if (part >= n_pieces) return;
   const int begin = part * piece, end = min(u.n, begin + piece);
@@ -768,7 +790,7 @@ __global__ void __launch_bounds__(kThreads, MB < 2 ? 3 : 2) ta_attend_kernel(ta_
     if (n_pieces == 1) {
       finish(r0 + r, j, mm, ll, x);
     } else {
-      const long long slot = ((long long)group * pieces + part) * R + r;
+      const long long slot = ((long long)group * cut.pieces + part) * R + r;
       *reinterpret_cast<float4*>(sc.part + slot * D + j) = x;
       if (j == 0) sc.part_ml[slot] = make_float2(mm, ll);
     }
@@ -788,7 +810,7 @@ __global__ void __launch_bounds__(kThreads, MB < 2 ? 3 : 2) ta_attend_kernel(ta_
   __threadfence();
   for (int w = tid; w < n_rows * (D / 4); w += kThreads) {
     const int r = w / (D / 4), j = (w - r * (D / 4)) * 4;
-    const long long slot = (long long)group * pieces * R + r;
+    const long long slot = (long long)group * cut.pieces * R + r;
     const float mm = joined_max(sc.part_ml + slot, n_pieces, R), from = mm == -INFINITY ? 0.0f : mm;
     float ll = 0.0f;
     float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -842,15 +864,18 @@ __global__ void __launch_bounds__(256) ta_attend_mass_kernel(ta_attend_args a, S
 // How a call is cut: query rows of a block, and pieces of the cache rows. Sized for the 148 SMs of a B200 at two (bf16, or 32
 // query rows) or three blocks each.
 struct Plan {
-  int mb, row_blocks, piece, pieces;
+  int mb, row_blocks, piece, pieces, target;
 };
-constexpr int kPieceUnit = 128;  // rows: whole rounds of every variant's four warps
+constexpr int kEvenBatch = 1024;  // sequences whose lengths every block adds up
 // The smallest number of pieces that fills whole rounds of resident blocks: a last round with few blocks costs as much as a full
 // one. bf16 is bound by memory and content with 85 % of a round, the 8-bit formats by instructions (95 %). us at 1, 2, 3, 4, 6, 8
 // pieces: 128 units of 32768 bf16 rows 563, 333, 441, 343, 349, 354; 288 units of 16384 e4m3 rows -, 312, 252, 257, 265, -.
+// Where every sequence has a length of its own, and all units fit at once, the pieces are cut on the device from the sum of the
+// lengths, with room for twice as many: 4 x 4 units of 100001 to 131072 int8 rows 154 us, 168 with pieces of max_len / 27; not with
+// more units (512 units of 2048 to 16384 e4m3 rows 308 and 294), whose empty blocks cost more than evenness brings.
 // With more units than fit at once lengths may differ: four rounds at least (512 units of 2048 to 16384 e4m3 rows
 // -, 331, 312, 293, 294, -; 296 units of 32768 bf16 rows alike lose 1.5 %, 726 to 737).
-Plan plan_of(long long units, int rows, int max_len, bool codes) {
+Plan plan_of(long long units, int rows, int max_len, bool codes, int ragged_batch) {
   Plan p;
   p.mb = rows <= 8 ? 0 : rows <= 16 ? 1 : 2;
   p.row_blocks = (rows + rows_of(p.mb) - 1) / rows_of(p.mb);
@@ -866,6 +891,11 @@ Plan plan_of(long long units, int rows, int max_len, bool codes) {
   p.piece = ((max_len + k - 1) / k + kPieceUnit - 1) / kPieceUnit * kPieceUnit;
   if (p.piece < kPieceUnit) p.piece = kPieceUnit;
   p.pieces = max_len > p.piece ? (max_len + p.piece - 1) / p.piece : 1;
+  p.target = 0;
+  if (p.pieces > 1 && ragged_batch > 1 && ragged_batch <= kEvenBatch && groups <= slots) {
+    p.target = (int)(groups * p.pieces);
+    p.pieces = 2 * p.pieces < most ? 2 * p.pieces : most;
+  }
   return p;
 }
 constexpr size_t up(size_t x) { return (x + 255) / 256 * 256; }
@@ -883,7 +913,8 @@ cudaError_t launch(const ta_attend_args& a, const Scratch& sc, const Plan& p, cu
     set[dev & 63] = true;
   }
   cfg.dynamicSmemBytes = smem;
-  return cudaLaunchKernelEx(&cfg, ta_attend_kernel<D, FMT, MB>, a, sc, p.pieces, p.piece, p.row_blocks, 128u, status);
+  return cudaLaunchKernelEx(&cfg, ta_attend_kernel<D, FMT, MB>, a, sc,
+                            Cut{p.pieces, p.piece, p.row_blocks, p.target, a.n_layers * a.cache.Hkv * p.row_blocks}, 128u, status);
 }
 template <int D, int FMT>
 cudaError_t launch(const ta_attend_args& a, const Scratch& sc, const Plan& p, cudaLaunchConfig_t& cfg, ta_dev_status* status) {
@@ -898,8 +929,9 @@ cudaError_t launch(const ta_attend_args& a, const Scratch& sc, const Plan& p, cu
   return launch<D, TA_CACHE_INT8>(a, sc, p, cfg, status);
 }
 
-size_t carve(long long units, int rows, int d, int max_len, bool codes, bool with_mass, uint8_t* base, Scratch* sc) {
-  const Plan p = plan_of(units, rows, max_len, codes);
+size_t carve(long long units, int rows, int d, int max_len, bool codes, int ragged_batch, bool with_mass, uint8_t* base,
+             Scratch* sc) {
+  const Plan p = plan_of(units, rows, max_len, codes, ragged_batch);
   const size_t slots = p.pieces > 1 ? (size_t)units * p.row_blocks * p.pieces * rows_of(p.mb) : 0;
   const long long stride = (max_len + 31) / 32 * 32;
   size_t off = 0;
@@ -922,16 +954,17 @@ size_t carve(long long units, int rows, int d, int max_len, bool codes, bool wit
 
 }  // namespace
 
-size_t ta_attend_scratch(int units, int rows, int d, int max_len, bool codes, bool with_mass) {
-  return carve(units, rows, d, max_len, codes, with_mass, nullptr, nullptr);
+size_t ta_attend_scratch(int units, int rows, int d, int max_len, bool codes, int ragged_batch, bool with_mass) {
+  return carve(units, rows, d, max_len, codes, ragged_batch, with_mass, nullptr, nullptr);
 }
 
 cudaError_t ta_launch_attend(const ta_attend_args& a, int* tickets, ta_dev_status* status, cudaStream_t stream) {
   const int units = a.n_layers * a.cache.batch * a.cache.Hkv, rows = a.Hq / a.cache.Hkv * a.T;
   const bool codes = a.cache.format != TA_CACHE_BF16;
-  const Plan p = plan_of(units, rows, a.max_len, codes);
+  const int ragged_batch = a.cache.lens && !a.cache.lens_per_unit ? a.cache.batch : 0;
+  const Plan p = plan_of(units, rows, a.max_len, codes, ragged_batch);
   Scratch sc;
-  carve(units, rows, a.d, a.max_len, codes, a.mass != nullptr, a.scratch, &sc);
+  carve(units, rows, a.d, a.max_len, codes, ragged_batch, a.mass != nullptr, a.scratch, &sc);
   sc.ticket = tickets;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((long long)units * p.row_blocks * p.pieces), 1, 1);

@@ -58,7 +58,8 @@ struct ta_attend_args {
   long long mass_stride;
   uint8_t* scratch;
 };
-size_t ta_attend_scratch(int units, int rows, int d, int max_len, bool codes, bool with_mass);
+// ragged_batch: sequences, where every one has a length of its own, else 0
+size_t ta_attend_scratch(int units, int rows, int d, int max_len, bool codes, int ragged_batch, bool with_mass);
 // tickets: kAttendTickets words, zero before and after
 cudaError_t ta_launch_attend(const ta_attend_args& a, int* tickets, ta_dev_status* status, cudaStream_t stream);
 
