@@ -21,6 +21,8 @@
 #include <cuda_fp16.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "ta_cache.cuh"
 #include "ta_sm100.cuh"
 
@@ -56,6 +58,14 @@ constexpr int smem_bytes() {
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ const void* at16(const void* base, uint32_t units) {  // base + 16 * units, in one product
+  uint64_t r;
+  asm("mad.wide.u32 %0, %1, 16, %2;" : "=l"(r) : "r"(units), "l"(base));
+  return reinterpret_cast<const void*>(r);
 }
 __device__ __forceinline__ void cp4(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
@@ -248,49 +258,70 @@ __global__ void __launch_bounds__(kThreads, MB < 2 ? 3 : 2) ta_attend_kernel(ta_
   const int tiles = (end - begin + TK - 1) / TK, mine = tiles > warp ? (tiles - warp + kWarps - 1) / kWarps : 0;
 
   // ---- the ring
+  constexpr uint32_t kAllRows = TK == 32 ? 0xffffffffu : (1u << TK) - 1;
   const uint8_t *k_base = c.k + u.l * c.sl + u.g * c.sh, *v_base = c.v + u.l * c.sl + u.g * c.sh;
   const uint32_t sp16 = (uint32_t)(c.sp >> 4), sr16 = (uint32_t)(c.sr >> 4);
   const uint32_t ring = smem_u32(smem) + warp * S::STAGES * S::STAGE;
   uint32_t* there_w = s_there + warp * S::STAGES;
-  uint32_t at_row = 0, at_scale = 0;  // this lane's row of the next tile, in units of 16 bytes, and its scale
-  bool at_there = false;
+  // A lane's row of a coming tile: its page's number is read a tile early and not looked at before the row is fetched.
+  int page_id = 0, page_row = 0;  // (-1: the lane has no row)
   auto look_up = [&](int i) {
     const int r = begin + (warp + i * kWarps) * TK + lane;
-    at_there = lane < TK && r < end;
-    if (at_there) {
-      const int j = c.page_shift >= 0 ? r >> c.page_shift : (int)((unsigned)r / (unsigned)c.page), in_page = r - j * c.page;
-      const int id = c.table ? c.table[u.b * (long long)c.wide + j] : u.b * c.wide + j;
-      at_there = id >= 0 && id < c.n_pages;
-      if (!at_there) ta_report_bounds(status, 33, u.b, r);
-      at_row = (uint32_t)id * sp16 + (uint32_t)in_page * sr16;
-      at_scale = (uint32_t)id * (uint32_t)c.ssp + (uint32_t)in_page * (uint32_t)c.ssr;
+    page_row = -1;
+    if (lane < TK && r < end) {
+      const int j = c.page_shift >= 0 ? r >> c.page_shift : (int)((unsigned)r / (unsigned)c.page);
+      page_row = r - j * c.page;
+      if (c.table) page_id = c.table[u.b * (long long)c.wide + j];
+      else page_id = u.b * c.wide + j;
+    }
+  };
+  uint32_t at_row = 0, at_scale = 0;  // in units of 16 bytes, and of the scale
+  bool at_there = false;
+  auto place = [&](int i) {
+    at_there = page_row >= 0 && page_id >= 0 && page_id < c.n_pages;
+    if (page_row >= 0 && !at_there) ta_report_bounds(status, 33, u.b, begin + (warp + i * kWarps) * TK + lane);
+    at_row = at_there ? (uint32_t)page_id * sp16 + (uint32_t)page_row * sr16 : 0u;
+    at_scale = at_there ? (uint32_t)page_id * (uint32_t)c.ssp + (uint32_t)page_row * (uint32_t)c.ssr : 0u;
+  };
+  // A lane's 16 bytes of a row are the same for all the tile's rows that it copies, CHUNKS / 32 rows apart. Swizzles: eight lanes
+  // that read 16 bytes each at a time meet all banks (keys: two rows and four chunks; values: eight rows of one chunk through
+  // ldmatrix, or, of codes, four even rows and two chunks).
+  constexpr int ROWS_AT_ONCE = 32 / S::CHUNKS;
+  const int my_row = lane / S::CHUNKS, my_chunk = lane % S::CHUNKS;
+  const uint8_t *k_lane = k_base + my_chunk * 16, *v_lane = v_base + my_chunk * 16;
+  const float *ks_base = c.ks + u.l * c.ssl + u.g * c.ssh, *vs_base = c.vs + u.l * c.ssl + u.g * c.ssh;
+  auto copy = [&](uint32_t dst, auto all) {  // all: every row is there
+    uint32_t there = 0;
+    if constexpr (!decltype(all)::value) there = __ballot_sync(0xffffffffu, at_there);
+#pragma unroll
+    for (int k = 0; k < TK / ROWS_AT_ONCE; ++k) {
+      const int row = k * ROWS_AT_ONCE + my_row;
+      const uint32_t at = __shfl_sync(0xffffffffu, at_row, row);
+      const int kx = S::CHUNKS >= 8 ? (row & 1) << 2 : 0;
+      const int vx = !CODES ? row & 7 : S::CHUNKS >= 8 ? ((row >> 1) & 3) << 1 : (row >> 1) & 3;
+      const uint32_t to_k = dst + row * S::ROW + ((my_chunk ^ kx) << 4), to_v = dst + S::TILE + row * S::ROW + ((my_chunk ^ vx) << 4);
+      if constexpr (decltype(all)::value) {
+        cp16(to_k, at16(k_lane, at));
+        cp16(to_v, at16(v_lane, at));
+      } else {  // (a row that is not there stands at the pool's start and is not read)
+        cp16(to_k, at16(k_lane, at), (there >> row) & 1);
+        cp16(to_v, at16(v_lane, at), (there >> row) & 1);
+      }
+    }
+    if constexpr (CODES) {
+      cp4(dst + 2 * S::TILE + lane * 4, ks_base + at_scale, at_there);
+      cp4(dst + 2 * S::TILE + TK * 4 + lane * 4, vs_base + at_scale, at_there);
     }
   };
   auto issue = [&](int i) {
     if (i < mine) {
       const int stage = i % S::STAGES;
       const uint32_t dst = ring + stage * S::STAGE;
+      place(i);
       const uint32_t there = __ballot_sync(0xffffffffu, at_there);
       if (lane == 0) there_w[stage] = there;
-#pragma unroll
-      for (int k = 0; k < TK * S::CHUNKS / 32; ++k) {
-        const int row = (k * 32 + lane) / S::CHUNKS, ch = (k * 32 + lane) % S::CHUNKS;
-        const long long off = (long long)__shfl_sync(0xffffffffu, at_there ? at_row : 0u, row) * 16 + ch * 16;
-        const bool is = (there >> row) & 1;  // (a row that is not there stands at the pool's start and is not read)
-        // swizzles: eight lanes that read 16 bytes each at a time meet all banks (keys: two rows and four chunks; values: eight
-        // rows of one chunk through ldmatrix, or, of codes, four even rows and two chunks)
-        const int kx = S::CHUNKS >= 8 ? (row & 1) << 2 : 0;
-        const int vx = !CODES ? row & 7 : S::CHUNKS >= 8 ? ((row >> 1) & 3) << 1 : (row >> 1) & 3;
-        cp16(dst + row * S::ROW + ((ch ^ kx) << 4), k_base + off, is);
-        cp16(dst + S::TILE + row * S::ROW + ((ch ^ vx) << 4), v_base + off, is);
-      }
-      if constexpr (CODES) {
-        if (lane < TK) {
-          const long long src = u.l * c.ssl + u.g * c.ssh + (at_there ? at_scale : 0u);
-          cp4(dst + 2 * S::TILE + lane * 4, c.ks + src, at_there);
-          cp4(dst + 2 * S::TILE + TK * 4 + lane * 4, c.vs + src, at_there);
-        }
-      }
+      if (there == kAllRows) copy(dst, std::true_type{});
+      else copy(dst, std::false_type{});
       look_up(i + 1);
     }
     cp_commit();
@@ -462,7 +493,7 @@ __global__ void __launch_bounds__(kThreads, MB < 2 ? 3 : 2) ta_attend_kernel(ta_
     const int stage = i % S::STAGES, first = begin + (warp + i * kWarps) * TK;
     const uint32_t kt = ring + stage * S::STAGE, vt = kt + S::TILE, st = kt + 2 * S::TILE;
     const uint32_t there = there_w[stage];
-    const bool whole = there == (TK == 32 ? 0xffffffffu : (1u << TK) - 1) && first + TK <= seen_by_all;
+    const bool whole = there == kAllRows && first + TK <= seen_by_all;
 
     // ---- scores
     float s[MBN][NT][4];
