@@ -188,6 +188,7 @@ __device__ __forceinline__ Unit unit_of(const ta_attend_args& a, int unit, bool 
   return u;
 }
 
+constexpr int kJoined = 4096;    // pieces of a row block, times its rows: what the last block joins in shared memory
 constexpr int kPieceUnit = 128;  // cache rows: whole rounds of every variant's four warps
 struct Cut {                     // how the kernel's blocks share the cache rows of a unit's row block
   int pieces, piece, row_blocks;
@@ -202,12 +203,6 @@ struct Scratch {    // of one call (null: not used)
   float2* row_ml;   // [unit][row]: maximum and 1 / sum for the attention mass
   long long score_stride;
 };
-
-__device__ __forceinline__ float joined_max(const float2* ml, int parts, long long stride) {
-  float m = -INFINITY;
-  for (int i = 0; i < parts; ++i) m = fmaxf(m, __ldcg(&ml[i * stride].x));
-  return m;
-}
 
 // blockIdx.x = (unit * row blocks + block) * pieces + piece
 template <int D, int FMT, int MB>
@@ -839,25 +834,44 @@ __global__ void __launch_bounds__(kThreads, MB < 2 ? 3 : 2) ta_attend_kernel(ta_
   __syncthreads();
   if (!*s_last) return;
   __threadfence();
+  const long long at0 = (long long)group * cut.pieces * R;
+  float2* s_w = reinterpret_cast<float2*>(smem);  // [piece][row], at most kJoined of them: maximum and sum, then what a piece weighs
+  for (int r = warp; r < n_rows; r += kWarps) {   // a warp per row
+    const float2* ml = sc.part_ml + at0 + r;
+    float mm = -INFINITY, ll = 0.0f;
+    for (int k = lane; k < n_pieces; k += 32) {
+      const float2 p = __ldcg(&ml[(long long)k * R]);
+      s_w[k * R + r] = p;
+      mm = fmaxf(mm, p.x);
+    }
+#pragma unroll
+    for (int w = 16; w > 0; w >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, w));
+    const float from = mm == -INFINITY ? 0.0f : mm;
+    for (int k = lane; k < n_pieces; k += 32) {
+      const float2 p = s_w[k * R + r];
+      const float f = p.y == 0.0f ? 0.0f : ex2(p.x - from);
+      s_w[k * R + r].x = f;
+      if (p.y != 0.0f) ll += p.y * f;
+    }
+#pragma unroll
+    for (int w = 16; w > 0; w >>= 1) ll += __shfl_xor_sync(0xffffffffu, ll, w);
+    if (lane == 0) s_ml[r] = make_float2(mm, ll);
+  }
+  __syncthreads();
   for (int w = tid; w < n_rows * (D / 4); w += kThreads) {
     const int r = w / (D / 4), j = (w - r * (D / 4)) * 4;
-    const long long slot = (long long)group * cut.pieces * R + r;
-    const float mm = joined_max(sc.part_ml + slot, n_pieces, R), from = mm == -INFINITY ? 0.0f : mm;
-    float ll = 0.0f;
+    const float* part_of = sc.part + (at0 + r) * D + j;
     float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
+#pragma unroll 8
     for (int k = 0; k < n_pieces; ++k) {
-      const float2 ml = __ldcg(&sc.part_ml[slot + (long long)k * R]);
-      const float4 y = __ldcg(reinterpret_cast<const float4*>(sc.part + (slot + (long long)k * R) * D + j));
-      const float f = ml.y == 0.0f ? 0.0f : ex2(ml.x - from);
-      if (ml.y == 0.0f) continue;
-      ll += ml.y * f;
+      const float4 y = __ldcg(reinterpret_cast<const float4*>(part_of + (long long)k * R * D));
+      const float f = s_w[k * R + r].x;
       x.x += y.x * f;
       x.y += y.y * f;
       x.z += y.z * f;
       x.w += y.w * f;
     }
-    finish(r0 + r, j, mm, ll, x);
+    finish(r0 + r, j, s_ml[r].x, s_ml[r].y, x);
   }
 }
 
@@ -911,7 +925,8 @@ Plan plan_of(long long units, int rows, int max_len, bool codes, int ragged_batc
   p.mb = rows <= 8 ? 0 : rows <= 16 ? 1 : 2;
   p.row_blocks = (rows + rows_of(p.mb) - 1) / rows_of(p.mb);
   const long long groups = units * p.row_blocks, slots = 148 * (p.mb < 2 ? 3 : 2);
-  const int most = groups > kAttendTickets ? 1 : max_len <= kPieceUnit ? 1 : (max_len + kPieceUnit - 1) / kPieceUnit;
+  int most = groups > kAttendTickets || max_len <= kPieceUnit ? 1 : (max_len + kPieceUnit - 1) / kPieceUnit;
+  if (most > kJoined / rows_of(p.mb)) most = kJoined / rows_of(p.mb);
   int k = 1;
   for (; k < most; ++k) {
     const long long blocks = groups * k, rounds = (blocks + slots - 1) / slots;
@@ -934,6 +949,7 @@ constexpr size_t up(size_t x) { return (x + 255) / 256 * 256; }
 template <int D, int FMT, int MB>
 cudaError_t launch(const ta_attend_args& a, const Scratch& sc, const Plan& p, cudaLaunchConfig_t& cfg, ta_dev_status* status) {
   constexpr int smem = smem_bytes<D, FMT, MB>();
+  static_assert(Shape<D, FMT>::RING >= kJoined * 8, "the join's weights take the ring's place");
   static bool set[64] = {};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
