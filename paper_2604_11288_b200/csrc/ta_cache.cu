@@ -1,10 +1,13 @@
 // Writing new keys and values into a cache, in its format, and reading rows back.
 //
-// Both move every row once: 2 d bytes of bf16 on one side and 2 d or d + 4 on the other, for a handful of operations an
-// element; memory is the bound. A row is held by d / 8 lanes, 16 bytes of bf16 each (8 of codes), so a warp holds two rows
-// (d = 128) or four; a thread has kRows rows of k and of v on their way at once. The largest magnitude of a row meets in
-// three or four shuffles. Keys that are rotated: the angles of a block's tokens are formed once, for all heads, in shared memory;
-// a lane's partner coordinates (half layout) come by shuffles.
+// Both move every row once: 2 d bytes of bf16 on one side and 2 d or d + 4 on the other, for some operations an element; memory
+// is the bound where the instructions stay under about 130 a row and warp. A row is held by d / 8 lanes, 16 bytes of bf16 each
+// (8 of codes), so a warp holds two rows (d = 128) or four. What does not depend on a lane is found once, by a thread per row,
+// and handed on in shared memory: where the row lies (kept per lane: 4382 us where this takes 2266, both without the next
+// two), angles of the tokens (for all heads), and of a row's keys and values only one lane's division each. The largest magnitude of a
+// row meets in three or four shuffles; a lane's partner coordinates (half layout) come by four of packed pairs.
+// 2 x 16 x 32768 tokens of 8 heads, written and read: bf16 2632 us, 6.5 TB/s; e4m3 2044, 6.4 TB/s; rotated on the way bf16 2691,
+// 6.4 TB/s, e4m3 2662, 4.9 TB/s (bound by instructions: issue slots 74 % taken).
 #include <math.h>
 
 #include "ta_cache.cuh"
@@ -12,8 +15,8 @@
 namespace {
 
 constexpr int kThreads = 128;
-// Rows of k, and of v, of a block: 32 keep memory busy (16: 2989 us where 32 take 2722, see below), 8 spread a call with few
-// rows over more SMs.
+// Rows of k, and of v, of a block: 32 keep memory busy (16: 2989 us where 32 take 2722, rotated into e4m3 and read), 8 spread a call
+// with few rows over more SMs (64 tokens of 8 heads 6.9 us, 11.6 with 32).
 constexpr int kItems = 32, kFewItems = 8;
 constexpr long long kFewRows = 148 * 32;
 
@@ -114,8 +117,12 @@ __global__ void __launch_bounds__(kThreads, 8) ta_cache_append_kernel(ta_cache_m
   ta_launch_dependents();
   constexpr int N = Lanes<D>::N, GROUPS = Lanes<D>::GROUPS, PER = ITEMS / GROUPS;
   constexpr bool CODES = FMT != TA_CACHE_BF16;
+  // positions looked up once a token, behind the places (2662 us, beside them 2870), or, in a call with few rows, once an angle,
+  // beside them (64 tokens 7.1 us, 7.4 behind)
+  constexpr bool ONCE = ITEMS == kItems;
   extern __shared__ float2 s_cs[];  // [token][pair]
   __shared__ Place s_place[ITEMS];
+  __shared__ int s_position[ITEMS];
   __shared__ Kept s_kept;
   const ta_cache_dev& c = a.cache;
   const int lane = threadIdx.x % N, group = threadIdx.x / N, l = blockIdx.y, half = a.rot.d_rot / 2;
@@ -145,9 +152,9 @@ __global__ void __launch_bounds__(kThreads, 8) ta_cache_append_kernel(ta_cache_m
       if (++g == c.Hkv) g = 0, ++tok;
     }
   }
-  keep(s_kept, a.seq, c, !a.rows || TURN);
+  keep(s_kept, a.seq, c, true);
   __syncthreads();
-  // one thread finds an item's place, while the others form the angles
+  // one thread finds an item's place
   if (threadIdx.x < todo) {
     const unsigned w = first + threadIdx.x, tok = w / c.Hkv;
     const int g = (int)(w - tok * c.Hkv);
@@ -160,15 +167,20 @@ __global__ void __launch_bounds__(kThreads, 8) ta_cache_append_kernel(ta_cache_m
     p.row = at.row < 0 ? -1 : l * c.sl + g * c.sh + at.row;
     p.scale = l * c.ssl + g * c.ssh + at.scale;
     s_place[threadIdx.x] = p;
+    // without positions a token's is its row, the same for all layers and heads
+    if constexpr (TURN && ONCE) s_position[tok - tok0] = a.rot.positions ? a.rot.positions[tok] : (int)row;
   }
+  if constexpr (TURN && ONCE) __syncthreads();
   if constexpr (TURN) {
     for (unsigned w = kThreads - 1 - threadIdx.x; w < tokens * half; w += kThreads) {
-      const unsigned i = w / half, p = w - i * half, tok = tok0 + i;
+      const unsigned i = w / half, p = w - i * half;
       int position;
-      if (a.rot.positions) {
-        position = a.rot.positions[tok];
+      if constexpr (ONCE) {
+        position = s_position[i];
+      } else if (a.rot.positions) {
+        position = a.rot.positions[tok0 + i];
       } else {
-        const Token t = token_of(s_kept, a.seq, tok);  // the row, the same for all layers and heads
+        const Token t = token_of(s_kept, a.seq, tok0 + i);
         position = len_of(s_kept, a.seq, c, l, t.b, 0) + t.i;
       }
       s_cs[w] = ta_cos_sin(a.rot, a.rot.phase[p], position);
