@@ -521,7 +521,7 @@ ta_status ta_rotate(ta_ctx* ctx, const ta_batch* batch, int Hq, int Hkv, int d, 
  *   k + l*stride_l + page_id*stride_p + g*stride_h + (r % page)*stride_r   (elements; v likewise, scales with their own)
  * table NULL: the sequence's pages are b * pages_per_seq + r / page (with page rows a sequence: one dense row block each).
  * Strides in elements, multiples of 16 bytes (scale strides: any), not negative; k and v 16-byte aligned; d 64 or 128. What
- * a table holds behind the pages that a call reaches is not read. The pages of one layer and head span less than 64 GiB and
+ * a table holds behind the pages that a call reaches has no influence. The pages of one layer and head span less than 64 GiB and
  * 2^32 scales, layers and heads as much as they like. */
 enum { TA_CACHE_BF16 = 0, TA_CACHE_E4M3 = 1, TA_CACHE_INT8 = 2 };
 typedef struct ta_cache {

@@ -174,18 +174,16 @@ __device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) <
 struct Unit {
   int l, b, g, n;  // n: rows that are there
 };
-__device__ __forceinline__ Unit unit_of(const ta_attend_args& a, int unit, bool report, ta_dev_status* status) {
+__device__ __forceinline__ Unit unit_of(const ta_attend_args& a, int unit) {  // n still to come
   const ta_cache_dev& c = a.cache;
-  Unit u;
-  u.g = unit % c.Hkv;
-  const int lb = unit / c.Hkv;
-  u.b = lb % c.batch;
-  u.l = lb / c.batch;
-  const long long asked = (long long)ta_cache_len(c, u.l, u.b, u.g) + a.new_rows;
-  const long long most = min((long long)a.max_len, (long long)c.wide * c.page);
+  const int lb = unit / c.Hkv, l = lb / c.batch;
+  return {l, lb - l * c.batch, unit - lb * c.Hkv, 0};
+}
+__device__ __forceinline__ int rows_of_unit(const ta_attend_args& a, const Unit& u, int len, bool report, ta_dev_status* status) {
+  const long long asked = (long long)len + a.new_rows;
+  const long long most = min((long long)a.max_len, (long long)a.cache.wide * a.cache.page);
   if (asked > most && report) ta_report_bounds(status, 32, u.b, (int)min(asked, 0x7fffffffLL));
-  u.n = (int)max(0LL, min(asked, most));
-  return u;
+  return (int)max(0LL, min(asked, most));
 }
 
 constexpr int kJoined = 4096;    // pieces of a row block, times its rows: what the last block joins in shared memory
@@ -229,8 +227,23 @@ __global__ void __launch_bounds__(kThreads, MB < 2 ? 3 : 2) ta_attend_kernel(ta_
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3;
   const int group = blockIdx.x / cut.pieces, part = blockIdx.x - group * cut.pieces;
   const int unit = group / cut.row_blocks, r0 = (group - unit * cut.row_blocks) * R;
-  const Unit u = unit_of(a, unit, part == 0 && r0 == 0 && tid == 0, status);
+  Unit u = unit_of(a, unit);
   const int G = a.Hq / c.Hkv, rows = G * a.T;
+  const int len = ta_cache_len(c, u.l, u.b, u.g);
+  // A lane's row of a coming tile: its page's number is read a tile early, the first one's beside the length, and not looked at
+  // before the row is fetched.
+  int page_id = 0, page_row = 0;
+  auto look_up = [&](int r) {
+    const int j = c.page_shift >= 0 ? r >> c.page_shift : (int)((unsigned)r / (unsigned)c.page);
+    page_row = r - j * c.page;
+    page_id = -1;
+    if (j < c.wide) {
+      if (c.table) page_id = c.table[u.b * (long long)c.wide + j];
+      else page_id = u.b * c.wide + j;
+    }
+  };
+  if (!cut.target) look_up(part * cut.piece + warp * TK + lane);
+  u.n = rows_of_unit(a, u, len, part == 0 && r0 == 0 && tid == 0, status);
   int piece = cut.piece;
   if (cut.target) {  // pieces of all sequences' rows shared out evenly, not of max_len
     const int most = (int)min((long long)a.max_len, (long long)c.wide * c.page);
@@ -258,23 +271,13 @@ __global__ void __launch_bounds__(kThreads, MB < 2 ? 3 : 2) ta_attend_kernel(ta_
   const uint32_t sp16 = (uint32_t)(c.sp >> 4), sr16 = (uint32_t)(c.sr >> 4);
   const uint32_t ring = smem_u32(smem) + warp * S::STAGES * S::STAGE;
   uint32_t* there_w = s_there + warp * S::STAGES;
-  // A lane's row of a coming tile: its page's number is read a tile early and not looked at before the row is fetched.
-  int page_id = 0, page_row = 0;  // (-1: the lane has no row)
-  auto look_up = [&](int i) {
-    const int r = begin + (warp + i * kWarps) * TK + lane;
-    page_row = -1;
-    if (lane < TK && r < end) {
-      const int j = c.page_shift >= 0 ? r >> c.page_shift : (int)((unsigned)r / (unsigned)c.page);
-      page_row = r - j * c.page;
-      if (c.table) page_id = c.table[u.b * (long long)c.wide + j];
-      else page_id = u.b * c.wide + j;
-    }
-  };
+  auto row_at = [&](int i) { return begin + (warp + i * kWarps) * TK + lane; };  // the lane's row of the warp's i-th tile
   uint32_t at_row = 0, at_scale = 0;  // in units of 16 bytes, and of the scale
   bool at_there = false;
   auto place = [&](int i) {
-    at_there = page_row >= 0 && page_id >= 0 && page_id < c.n_pages;
-    if (page_row >= 0 && !at_there) ta_report_bounds(status, 33, u.b, begin + (warp + i * kWarps) * TK + lane);
+    const bool asked = lane < TK && row_at(i) < end;
+    at_there = asked && page_id >= 0 && page_id < c.n_pages;
+    if (asked && !at_there) ta_report_bounds(status, 33, u.b, row_at(i));
     at_row = at_there ? (uint32_t)page_id * sp16 + (uint32_t)page_row * sr16 : 0u;
     at_scale = at_there ? (uint32_t)page_id * (uint32_t)c.ssp + (uint32_t)page_row * (uint32_t)c.ssr : 0u;
   };
@@ -317,11 +320,11 @@ __global__ void __launch_bounds__(kThreads, MB < 2 ? 3 : 2) ta_attend_kernel(ta_
       if (lane == 0) there_w[stage] = there;
       if (there == kAllRows) copy(dst, std::true_type{});
       else copy(dst, std::false_type{});
-      look_up(i + 1);
+      look_up(row_at(i + 1));
     }
     cp_commit();
   };
-  look_up(0);
+  if (cut.target) look_up(row_at(0));
 #pragma unroll
   for (int i = 0; i < S::STAGES - 1; ++i) issue(i);
 
@@ -882,7 +885,8 @@ __global__ void __launch_bounds__(256) ta_attend_mass_kernel(ta_attend_args a, S
   ta_wait_for_prior_grid();
   ta_launch_dependents();
   const int unit = blockIdx.x, G = a.Hq / a.cache.Hkv, rows = G * a.T;
-  const int n = unit_of(a, unit, false, nullptr).n;
+  const Unit u = unit_of(a, unit);
+  const int n = rows_of_unit(a, u, ta_cache_len(a.cache, u.l, u.b, u.g), false, nullptr);
   const float2* row_ml = sc.row_ml + (long long)unit * rows;
   const float* score = sc.score + (long long)unit * rows * sc.score_stride;
   for (long long j = 4LL * (blockIdx.y * 256 + threadIdx.x); j < a.mass_stride; j += 1024LL * gridDim.y) {
