@@ -2,10 +2,10 @@
 //
 // A unit (layer, sequence, KV head) has R = (Hq / Hkv) * T query rows that read the same n cache rows, each once: 4 d R
 // operations for 4 d bytes (bf16), so up to some tens of query rows the cache's bytes are the bound, and everything below
-// serves to keep them coming. The cache rows of a unit are cut into pieces of `piece` rows, a block each; a block's four
-// warps take its tiles (16 or 32 rows) in turn, each with a ring of its own in shared memory that asynchronous 16-byte
-// copies fill two tiles ahead, so no warp waits for another before the end. Any page size and any strides: a lane looks up
-// one row of the next tile one tile early. Rows that are not there are filled with zeros and masked.
+// serves to keep them coming. The cache rows of a unit are cut into pieces, a block each; a block's warps take its tiles (16
+// or 32 rows) in turn, each with two slots of its own in shared memory that asynchronous 16-byte copies fill a tile ahead, so
+// no warp waits for another before the end. Any page size and any strides: a lane looks up one row of a tile a tile before
+// that. Rows that are not there are filled with zeros and masked.
 //
 // Per tile and warp: scores S = Q K^T on the tensor cores (m16n8k16, fp32 sums), a running maximum and sum per query row,
 // O = O + P V on the tensor cores with P straight from the score registers. Products have 8 to 32 rows: far too few for a
@@ -18,6 +18,13 @@
 // its probabilities, relative to the largest power of two among the scales so far. Probabilities and rotated queries
 // enter their products as a sum of two 16-bit parts, hi + lo: with up to 8 query rows the lower half of the 16-row product,
 // which would be empty, holds the lo parts at no cost (MB = 0); with more rows the lo parts are a second product.
+//
+// What bounds it. bf16: memory, 16 x 32768 rows of 8 heads in 306 us, 7.0 TB/s. 8-bit: instructions, 940 for a tile of 32 rows, of
+// which 384 turn codes into fp16 and 64 are products: 36 x 16384 e4m3 rows of 8 heads 225 us, 5.5 TB/s; with 16 query rows 1200 or so
+// (8 x 131072 int8 rows of 4 heads 289 us, 3.8 TB/s). Cache rows as the long side of the products (S^T = K Q^T, half of them and of the
+// accumulators, four blocks an SM instead of three) were slower, 275 us where this took 238: no fewer instructions, and less
+// distance between those that depend on one another. Tiles of 16 rows for codes: 297 for 251. Bulk copies for codes: 511 for 296 row by
+// row, 247 for 250 in runs of 16 rows.
 #include <cuda_fp16.h>
 #include <math.h>
 
@@ -31,10 +38,7 @@ namespace {
 using ta_sm100::ex2;
 using ta_sm100::smem_u32;
 
-constexpr int kWarps = 4;
-constexpr int kThreads = kWarps * 32;
-
-template <int D, int FMT>
+template <int D, int FMT, int W>  // W: warps of a block
 struct Shape {
   static constexpr bool CODES = FMT != TA_CACHE_BF16;
   static constexpr int ROW = D * (CODES ? 1 : 2);                 // bytes of a row
@@ -44,16 +48,16 @@ struct Shape {
   static constexpr int STAGE = 2 * TILE + (CODES ? 2 * TK * 4 : 0);
   static constexpr int STAGES = 2;
   static constexpr int KS = D / 16;                               // products along d
-  static constexpr int RING = kWarps * STAGES * STAGE;
+  static constexpr int RING = W * STAGES * STAGE;
 };
 __host__ __device__ constexpr int rows_of(int MB) { return MB == 0 ? 8 : 16 * MB; }  // query rows of a block
-template <int D, int FMT, int MB>
+template <int D, int FMT, int MB, int W>
 constexpr int smem_bytes() {
   constexpr int R = rows_of(MB);
   constexpr int q32 = R * D * 4;  // queries in fp32, then (MB > 0) their fragments, hi and lo, in the same place
-  constexpr int join = kWarps * R * (D + 4) * 4;
-  constexpr int ring = Shape<D, FMT>::RING > join ? Shape<D, FMT>::RING : join;
-  return ring + q32 + R * 4 /* row factors */ + kWarps * R * 8 /* maxima and sums */ + kWarps * Shape<D, FMT>::STAGES * 4 + 16;
+  constexpr int join = W * R * (D + 4) * 4;
+  constexpr int ring = Shape<D, FMT, W>::RING > join ? Shape<D, FMT, W>::RING : join;
+  return ring + q32 + R * 4 /* row factors */ + W * R * 8 /* maxima and sums */ + W * Shape<D, FMT, W>::STAGES * 4 + 16;
 }
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool there) {
@@ -203,10 +207,11 @@ struct Scratch {    // of one call (null: not used)
 };
 
 // blockIdx.x = (unit * row blocks + block) * pieces + piece
-template <int D, int FMT, int MB>
-__global__ void __launch_bounds__(kThreads, MB < 2 ? 3 : 2) ta_attend_kernel(ta_attend_args a, Scratch sc, Cut cut,
+template <int D, int FMT, int MB, int W>
+__global__ void __launch_bounds__(W * 32, (MB < 2 ? 12 : 8) / W) ta_attend_kernel(ta_attend_args a, Scratch sc, Cut cut,
                                                               uint32_t times128, ta_dev_status* status) {
-  using S = Shape<D, FMT>;
+  using S = Shape<D, FMT, W>;
+  constexpr int kWarps = W, kThreads = W * 32;
   constexpr bool CODES = S::CODES, NARROW = MB == 0;
   constexpr int TK = S::TK, NT = TK / 8, KS = S::KS, R = rows_of(MB), MBN = NARROW ? 1 : MB, NR = NARROW ? 1 : 2 * MB;
   constexpr int NJ = D / 8;  // 8-wide tiles of the output
@@ -729,12 +734,12 @@ __global__ void __launch_bounds__(kThreads, MB < 2 ? 3 : 2) ta_attend_kernel(ta_
           product(2 * j + 1, b[2], b[3]);
         }
       } else {
-        constexpr int W = D / 32;  // words of a lane's part of a row: D / 8 coordinates
-        uint32_t v[4][W];
+        constexpr int WORDS = D / 32;  // words of a lane's part of a row: D / 8 coordinates
+        uint32_t v[4][WORDS];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int key = kk * 16 + 2 * t4 + (e & 1) + (e >> 1) * 8;
-          if constexpr (W == 4) {
+          if constexpr (WORDS == 4) {
             const uint4 q = lds128(vt + key * S::ROW + ((g8 ^ (((key >> 1) & 3) << 1)) << 4));
             v[e][0] = q.x, v[e][1] = q.y, v[e][2] = q.z, v[e][3] = q.w;
           } else {
@@ -743,7 +748,7 @@ __global__ void __launch_bounds__(kThreads, MB < 2 ? 3 : 2) ta_attend_kernel(ta_
           }
         }
 #pragma unroll
-        for (int w = 0; w < W; ++w) {
+        for (int w = 0; w < WORDS; ++w) {
           uint32_t b0[4], b1[4];  // pairs of two rows, one coordinate each
           b0[0] = pair_of<FMT, 0>(v[0][w], v[1][w], times128), b0[1] = pair_of<FMT, 1>(v[0][w], v[1][w], times128);
           b0[2] = pair_of<FMT, 2>(v[0][w], v[1][w], times128), b0[3] = pair_of<FMT, 3>(v[0][w], v[1][w], times128);
@@ -910,10 +915,10 @@ __global__ void __launch_bounds__(256) ta_attend_mass_kernel(ta_attend_args a, S
   }
 }
 
-// How a call is cut: query rows of a block, and pieces of the cache rows. Sized for the 148 SMs of a B200 at two (bf16, or 32
+// How a call is cut: query rows and warps of a block, and pieces of the cache rows. Sized for the 148 SMs of a B200 at two (bf16, or 32
 // query rows) or three blocks each.
 struct Plan {
-  int mb, row_blocks, piece, pieces, target;
+  int mb, warps, row_blocks, piece, pieces, target;
 };
 constexpr int kEvenBatch = 1024;  // sequences whose lengths every block adds up
 // The smallest number of pieces that fills whole rounds of resident blocks: a last round with few blocks costs as much as a full
@@ -922,6 +927,9 @@ constexpr int kEvenBatch = 1024;  // sequences whose lengths every block adds up
 // Where every sequence has a length of its own, and all units fit at once, the pieces are cut on the device from the sum of the
 // lengths, with room for twice as many: 4 x 4 units of 100001 to 131072 int8 rows 154 us, 168 with pieces of max_len / 27; not with
 // more units (512 units of 2048 to 16384 e4m3 rows 308 and 294), whose empty blocks cost more than evenness brings.
+// Many short units: blocks of two warps, twice as many an SM, whose starts and ends weigh half as much (4096 units in a step, us with
+// four and two warps: 17 rows 54 and 40, 65 rows 74 and 59, 257 rows 128 and 122, 4097 rows 1418 and 1403; one warp 36, 53, 121); not where
+// lengths differ much, which longer blocks even out less (4096 units of 100 to 1000 e4m3 rows 165 and 171).
 // With more units than fit at once lengths may differ: four rounds at least (512 units of 2048 to 16384 e4m3 rows
 // -, 331, 312, 293, 294, -; 296 units of 32768 bf16 rows alike lose 1.5 %, 726 to 737).
 Plan plan_of(long long units, int rows, int max_len, bool codes, int ragged_batch) {
@@ -942,6 +950,7 @@ Plan plan_of(long long units, int rows, int max_len, bool codes, int ragged_batc
   if (p.piece < kPieceUnit) p.piece = kPieceUnit;
   p.pieces = max_len > p.piece ? (max_len + p.piece - 1) / p.piece : 1;
   p.target = 0;
+  p.warps = p.mb == 0 && p.pieces == 1 && groups >= 4 * slots && (ragged_batch == 0 || max_len <= 512) ? 2 : 4;
   if (p.pieces > 1 && ragged_batch > 1 && ragged_batch <= kEvenBatch && groups <= slots) {
     p.target = (int)(groups * p.pieces);
     p.pieces = 2 * p.pieces < most ? 2 * p.pieces : most;
@@ -950,28 +959,29 @@ Plan plan_of(long long units, int rows, int max_len, bool codes, int ragged_batc
 }
 constexpr size_t up(size_t x) { return (x + 255) / 256 * 256; }
 
-template <int D, int FMT, int MB>
+template <int D, int FMT, int MB, int W>
 cudaError_t launch(const ta_attend_args& a, const Scratch& sc, const Plan& p, cudaLaunchConfig_t& cfg, ta_dev_status* status) {
-  constexpr int smem = smem_bytes<D, FMT, MB>();
-  static_assert(Shape<D, FMT>::RING >= kJoined * 8, "the join's weights take the ring's place");
+  constexpr int smem = smem_bytes<D, FMT, MB, W>();
+  static_assert(W < 4 || Shape<D, FMT, W>::RING >= kJoined * 8, "the join's weights take the ring's place");
   static bool set[64] = {};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (!set[dev & 63]) {
-    e = cudaFuncSetAttribute(ta_attend_kernel<D, FMT, MB>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    e = cudaFuncSetAttribute(ta_attend_kernel<D, FMT, MB, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     set[dev & 63] = true;
   }
+  cfg.blockDim = dim3(W * 32, 1, 1);
   cfg.dynamicSmemBytes = smem;
-  return cudaLaunchKernelEx(&cfg, ta_attend_kernel<D, FMT, MB>, a, sc,
+  return cudaLaunchKernelEx(&cfg, ta_attend_kernel<D, FMT, MB, W>, a, sc,
                             Cut{p.pieces, p.piece, p.row_blocks, p.target, a.n_layers * a.cache.Hkv * p.row_blocks}, 128u, status);
 }
 template <int D, int FMT>
 cudaError_t launch(const ta_attend_args& a, const Scratch& sc, const Plan& p, cudaLaunchConfig_t& cfg, ta_dev_status* status) {
-  if (p.mb == 0) return launch<D, FMT, 0>(a, sc, p, cfg, status);
-  if (p.mb == 1) return launch<D, FMT, 1>(a, sc, p, cfg, status);
-  return launch<D, FMT, 2>(a, sc, p, cfg, status);
+  if (p.mb == 0) return p.warps == 2 ? launch<D, FMT, 0, 2>(a, sc, p, cfg, status) : launch<D, FMT, 0, 4>(a, sc, p, cfg, status);
+  if (p.mb == 1) return launch<D, FMT, 1, 4>(a, sc, p, cfg, status);
+  return launch<D, FMT, 2, 4>(a, sc, p, cfg, status);
 }
 template <int D>
 cudaError_t launch(const ta_attend_args& a, const Scratch& sc, const Plan& p, cudaLaunchConfig_t& cfg, ta_dev_status* status) {
@@ -1019,7 +1029,6 @@ cudaError_t ta_launch_attend(const ta_attend_args& a, int* tickets, ta_dev_statu
   sc.ticket = tickets;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((long long)units * p.row_blocks * p.pieces), 1, 1);
-  cfg.blockDim = dim3(kThreads, 1, 1);
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   ta_pdl_attribute(&attr[0]);
