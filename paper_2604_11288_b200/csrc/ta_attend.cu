@@ -345,26 +345,27 @@ __global__ void __launch_bounds__(W * 32, (MB < 2 ? 12 : 8) / W) ta_attend_kerne
   };
   // up to 8 rows that are not rotated go straight to the fragments, others to shared memory in fp32 first
   const bool straight = NARROW && !a.rot.phase;
+  const int n_rows = min(R, rows - r0);
   if (!straight) {
-    for (int w = tid; w < R * D; w += kThreads) {
-      const int r = w / D, j = w - r * D, row = r0 + r;
-      float v = 0.0f;
-      if (row < rows) {
-        const __nv_bfloat16* q = query(row);
-        v = __bfloat162float(q[j]);
-        if (a.rot.phase && j < a.rot.d_rot) {
-          const int half = a.rot.d_rot / 2;
-          const int position = a.rot.positions ? a.rot.positions[u.b * a.T + row / G] : u.n - a.T + row / G;
-          const bool second = a.rot.interleaved ? (j & 1) : j >= half;
-          const int p = a.rot.interleaved ? j >> 1 : (second ? j - half : j);
-          const int other = a.rot.interleaved ? j ^ 1 : (second ? j - half : j + half);
-          const float2 cs = ta_cos_sin(a.rot, a.rot.phase[p], position);
-          const float o = __bfloat162float(q[other]);
-          v = second ? o * cs.y + v * cs.x : v * cs.x - o * cs.y;
-        }
-      }
-      s_q[w] = v;
+    const int half = a.rot.phase ? a.rot.d_rot / 2 : 0, rest = (D - 2 * half) / 4;  // pairs, and fours that are not rotated
+    for (int w = tid; w < n_rows * half; w += kThreads) {
+      const int r = w / half, p = w - r * half, row = r0 + r;
+      const int c0 = a.rot.interleaved ? 2 * p : p, c1 = a.rot.interleaved ? 2 * p + 1 : p + half;
+      const __nv_bfloat16* q = query(row);
+      const float x = __bfloat162float(q[c0]), y = __bfloat162float(q[c1]);
+      const int position = a.rot.positions ? a.rot.positions[u.b * a.T + row / G] : u.n - a.T + row / G;
+      const float2 cs = ta_cos_sin(a.rot, a.rot.phase[p], position);
+      s_q[r * D + c0] = x * cs.x - y * cs.y;
+      s_q[r * D + c1] = x * cs.y + y * cs.x;
     }
+    for (int w = tid; w < n_rows * rest; w += kThreads) {
+      const int r = w / rest, c0 = 2 * half + (w - r * rest) * 4;
+      const uint2 x = *reinterpret_cast<const uint2*>(query(r0 + r) + c0);
+      const float2 lo = unpack2<false>(x.x), hi = unpack2<false>(x.y);
+      *reinterpret_cast<float4*>(s_q + r * D + c0) = make_float4(lo.x, lo.y, hi.x, hi.y);
+    }
+    for (int w = tid + n_rows * (D / 4); w < R * (D / 4); w += kThreads)
+      reinterpret_cast<float4*>(s_q)[w] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     __syncthreads();
   }
   // a row's part of four coordinates for product ks: the order in which a lane's bytes of a key row come
@@ -801,7 +802,6 @@ __global__ void __launch_bounds__(W * 32, (MB < 2 ? 12 : 8) / W) ta_attend_kerne
       if (sc.row_ml) sc.row_ml[(long long)unit * rows + row] = make_float2(mm, inv);
     }
   };
-  const int n_rows = min(R, rows - r0);
   for (int w = tid; w < n_rows * (D / 4); w += kThreads) {
     const int r = w / (D / 4), j = (w - r * (D / 4)) * 4;
     float mm = -INFINITY, ll = 0.0f;
