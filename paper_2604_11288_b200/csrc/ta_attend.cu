@@ -891,20 +891,55 @@ __global__ void __launch_bounds__(W * 32, (MB < 2 ? 12 : 8) / W) ta_attend_kerne
     }
   }
   __syncthreads();
-  for (int w = tid; w < n_rows * (D / 4); w += kThreads) {
-    const int r = w / (D / 4), j = (w - r * (D / 4)) * 4;
-    const float* part_of = sc.part + (at0 + r) * D + j;
-    float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 8
-    for (int k = 0; k < n_pieces; ++k) {
-      const float4 y = __ldcg(reinterpret_cast<const float4*>(part_of + (long long)k * R * D));
-      const float f = s_w[k * R + r].x;
-      x.x += y.x * f;
-      x.y += y.y * f;
-      x.z += y.z * f;
-      x.w += y.w * f;
+  if constexpr (R > 8) {
+    // A thread has four coordinates of every LANES-th row, and all their loads on their way: none under a condition (rows and pieces
+    // that are not there repeat the last one, with no weight), nothing stored before the last.
+    constexpr int LANES = kThreads / (D / 4), ITEMS = R / LANES, AHEAD = 16 / ITEMS < 4 ? 4 : 16 / ITEMS;
+    const int r_first = tid / (D / 4), j = tid % (D / 4) * 4;
+    float4 x[ITEMS];
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) x[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    const float* part_of = sc.part + at0 * D + j;
+    for (int k0 = 0; k0 < n_pieces; k0 += AHEAD) {
+      float4 y[AHEAD][ITEMS];
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+          y[k][i] = __ldcg(reinterpret_cast<const float4*>(
+              part_of + ((long long)min(k0 + k, n_pieces - 1) * R + min(r_first + i * LANES, n_rows - 1)) * D));
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+          const float f = k0 + k < n_pieces ? s_w[(k0 + k) * R + r_first + i * LANES].x : 0.0f;
+          x[i].x += y[k][i].x * f;
+          x[i].y += y[k][i].y * f;
+          x[i].z += y[k][i].z * f;
+          x[i].w += y[k][i].w * f;
+        }
     }
-    finish(r0 + r, j, s_ml[r].x, s_ml[r].y, x);
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      const int r = r_first + i * LANES;
+      if (r < n_rows) finish(r0 + r, j, s_ml[r].x, s_ml[r].y, x[i]);
+    }
+  } else {
+    for (int w = tid; w < n_rows * (D / 4); w += kThreads) {
+      const int r = w / (D / 4), j = (w - r * (D / 4)) * 4;
+      const float* part_of = sc.part + (at0 + r) * D + j;
+      float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+      for (int k = 0; k < n_pieces; ++k) {
+        const float4 y = __ldcg(reinterpret_cast<const float4*>(part_of + (long long)k * R * D));
+        const float f = s_w[k * R + r].x;
+        x.x += y.x * f;
+        x.y += y.y * f;
+        x.z += y.z * f;
+        x.w += y.w * f;
+      }
+      finish(r0 + r, j, s_ml[r].x, s_ml[r].y, x);
+    }
   }
 }
 
