@@ -844,8 +844,8 @@ __global__ void __launch_bounds__(W * 32, (MB < 2 ? 12 : 8) / W) ta_attend_kerne
   __threadfence();
   const long long at0 = (long long)group * cut.pieces * R;
   float2* s_w = reinterpret_cast<float2*>(smem);  // [piece][row], at most kJoined of them: maximum and sum, then what a piece weighs
-  // Lanes that share a row, all rows at once: a warp per row takes four or eight rows one after another (one unit's 32 query rows
-  // over 129 to 4096 rows 23 to 38 us, so 19 to 33). With 8 rows a warp has two at most, and the plainer code leaves the loop faster
+  // Lanes that share a row, all rows at once: a warp per row takes four or eight rows one after another (8 units' 32 query rows
+  // over 129 to 4096 rows 23 to 38 us, so 19 to 33, and 18 to 27 with the loads below). With 8 rows a warp has two at most, and the plainer code leaves the loop faster
   // (64 ragged conversations in e4m3 264 us, 281 with the other).
   if constexpr (R > 8) {
 #pragma unroll 4
@@ -985,7 +985,7 @@ constexpr int kEvenBatch = 1024;  // sequences whose lengths every block adds up
 // one. bf16 is bound by memory and content with 85 % of a round, the 8-bit formats by instructions (95 %). us at 1, 2, 3, 4, 6, 8
 // pieces: 128 units of 32768 bf16 rows 563, 333, 441, 343, 349, 354; 288 units of 16384 e4m3 rows -, 312, 252, 257, 265, -.
 // Where every sequence has a length of its own, and all units fit at once, the pieces are cut on the device from the sum of the
-// lengths, with room for twice as many: 4 x 4 units of 100001 to 131072 int8 rows 154 us, 168 with pieces of max_len / 27; not with
+// lengths, with room for twice as many: 4 x 4 units of 100001 to 131072 int8 rows 154 us, 168 with pieces of max_len / 27 (127 by now); not with
 // more units (512 units of 2048 to 16384 e4m3 rows 308 and 294), whose empty blocks cost more than evenness brings.
 // Many short units: blocks of two warps, twice as many an SM, whose starts and ends weigh half as much (4096 units in a step, us with
 // four and two warps: 17 rows 54 and 40, 65 rows 74 and 59, 257 rows 128 and 122, 4097 rows 1418 and 1403; one warp 36, 53, 121); not where
