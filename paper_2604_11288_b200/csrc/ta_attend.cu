@@ -15,7 +15,7 @@
 //
 // Precision. bf16 caches: products of bf16 values. 8-bit caches: codes are exact in fp16; queries are scaled per row by a power
 // of two into fp16's range (and back in the score's factor), the scale of a key row multiplies its scores, that of a value row
-// its probabilities, relative to the largest power of two among the scales so far. Probabilities and rotated queries
+// its probabilities, relative to a power of two that is a query row's own. Probabilities and rotated queries
 // enter their products as a sum of two 16-bit parts, hi + lo: with up to 8 query rows the lower half of the 16-row product,
 // which would be empty, holds the lo parts at no cost (MB = 0); with more rows the lo parts are a second product.
 //
@@ -488,7 +488,14 @@ __global__ void __launch_bounds__(W * 32, (MB < 2 ? 12 : 8) / W) ta_attend_kerne
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[i][j][e] = 0.0f;
-  int ref = -100;  // 8-bit caches: exponent that the value rows' scales are taken relative to
+  // 8-bit caches: exponents that probabilities times value rows' scales are taken relative to, at least kLeastRef (the smallest scale
+  // that ta_cache_append writes is above 2^-109)
+  constexpr int kLeastRef = -112;
+  int ref[CODES ? NR : 1];
+  if constexpr (CODES) {
+#pragma unroll
+    for (int r = 0; r < NR; ++r) ref[r] = kLeastRef;
+  }
 
   for (int i = 0; i < mine; ++i) {
     cp_wait<S::STAGES - 2>();
@@ -576,7 +583,10 @@ __global__ void __launch_bounds__(W * 32, (MB < 2 ? 12 : 8) / W) ta_attend_kerne
           const bool is = (there >> k) & 1;
 #pragma unroll
           for (int r = 0; r < NR; ++r)
-            if (!is || first + k >= limit[r]) x[r][y][e] = -INFINITY;
+            if (!is || first + k >= limit[r]) {
+              x[r][y][e] = -INFINITY;
+              if constexpr (CODES && NARROW) (e ? vs[y].y : vs[y].x) = 0.0f;  // (may be NaN)
+            }
         }
     }
     if (sc.score) {
@@ -604,6 +614,7 @@ __global__ void __launch_bounds__(W * 32, (MB < 2 ? 12 : 8) / W) ta_attend_kerne
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
       const float from = top == -INFINITY ? 0.0f : top;
       keep[r] = ex2(m[r] - from);
+      const int fell = CODES ? (int)fminf(from - m[r], 512.0f) : 0;  // whole bits by which what came before is taken down
       grew |= top > m[r];
       m[r] = top;
       float sum = 0.0f;
@@ -614,34 +625,54 @@ __global__ void __launch_bounds__(W * 32, (MB < 2 ? 12 : 8) / W) ta_attend_kerne
         sum += x[r][y][0] + x[r][y][1];
       }
       l[r] = l[r] * keep[r] + sum;
+      if constexpr (CODES) {
+        ref[r] -= fell;
+        keep[r] *= pow2(min(fell, 126));
+      }
     }
     if constexpr (CODES) {
-      // probabilities times their value rows' scales, relative to 2^ref and times 2^14: at most 2^15, and 2^-38 of the largest
-      // is still told from zero. Scales that are not finite set no reference.
-      uint32_t top = lane < TK ? lds32(st + (TK + lane) * 4) & 0x7fffffffu : 0;
-      top = __reduce_max_sync(0xffffffffu, top >= 0x7f800000u ? 0 : top);
-      const int e = (int)(top >> 23) - 127;
-      if (e > ref) {
-        const float down = ref - e < -126 ? 0.0f : pow2(ref - e);
+      // Probabilities times their value rows' scales, for each query row relative to 2^ref, the largest that it has met (in the frame
+      // of its running maximum), and times 2^14: at most 2^15, and 2^-38 of the largest is still told from zero. A scale that a
+      // row does not see, or sees with next to no probability, takes nothing from the others, however large it is. (One reference for
+      // all rows of a warp, from the scales alone, let such a scale wipe out what the other rows hold. A query row's own costs 2 to 4 %
+      // with more than 8 rows and nothing with fewer.)
+      if (NARROW || whole) {
 #pragma unroll
-        for (int r = 0; r < NR; ++r) keep[r] *= down;
-        ref = e;
-        grew = true;
-      }
-      const float up = pow2(min(14 - ref, 127));
+        for (int r = 0; r < NR; ++r)
 #pragma unroll
-      for (int y = 0; y < NT; ++y) {
-        vs[y].x *= up;
-        vs[y].y *= up;
-#pragma unroll
-        for (int r = 0; r < NR; ++r) {
-          if (whole) {
+          for (int y = 0; y < NT; ++y) {
             x[r][y][0] *= vs[y].x;
             x[r][y][1] *= vs[y].y;
-          } else {  // a scale that is not seen may be NaN
-            x[r][y][0] = x[r][y][0] == 0.0f ? 0.0f : x[r][y][0] * vs[y].x;
-            x[r][y][1] = x[r][y][1] == 0.0f ? 0.0f : x[r][y][1] * vs[y].y;
           }
+      } else {
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+          for (int y = 0; y < NT; ++y)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int k = y * 8 + 2 * t4 + e;
+              x[r][y][e] *= e ? vs[y].y : vs[y].x;
+              if (!((there >> k) & 1) || first + k >= limit[r]) x[r][y][e] = 0.0f;  // (its scale may be NaN)
+            }
+      }
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {
+        float top = 0.0f;
+#pragma unroll
+        for (int y = 0; y < NT; ++y) top = fmaxf(top, fmaxf(fabsf(x[r][y][0]), fabsf(x[r][y][1])));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const int now = max(max(ref[r], (int)(__float_as_uint(top) >> 23) - 127), kLeastRef);
+        const int by = now - ref[r];
+        keep[r] *= by > 126 ? 0.0f : pow2(-by);
+        grew |= by != 0;
+        ref[r] = now;
+        const float up = pow2(14 - now);
+#pragma unroll
+        for (int y = 0; y < NT; ++y) {
+          x[r][y][0] *= up;
+          x[r][y][1] *= up;
         }
       }
     }
@@ -767,7 +798,6 @@ __global__ void __launch_bounds__(W * 32, (MB < 2 ? 12 : 8) / W) ta_attend_kerne
   __syncthreads();  // the rings are free
   constexpr int LD = D + 4;
   float* s_o = reinterpret_cast<float*>(smem);
-  const float unit_of_o = CODES ? pow2(max(ref - 14 + kCodeUnit<FMT>, -126)) : 1.0f;
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
     l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
@@ -776,6 +806,8 @@ __global__ void __launch_bounds__(W * 32, (MB < 2 ? 12 : 8) / W) ta_attend_kerne
     if (t4 == 0) s_ml[warp * R + row] = make_float2(m[r], l[r]);
     if (r0 + row >= rows) continue;
     float* to = s_o + (warp * R + row) * LD;
+    float unit_of_o = 1.0f;
+    if constexpr (CODES) unit_of_o = pow2(ref[r] - 14 + kCodeUnit<FMT>);
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
       const float v0 = NARROW ? o[0][j][0] + o[0][j][2] : o[r / 2][j][(r & 1) * 2];
