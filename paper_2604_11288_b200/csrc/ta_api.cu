@@ -1264,7 +1264,10 @@ ta_status ta_attend_scratch_bytes(const ta_cache* cache, int Hq, int T, int max_
   if (!out_bytes) return TA_ERR_INVALID_ARG;
   ta_status s = check_attend(cache, Hq, T, max_len);
   if (s != TA_OK) return s;
-  *out_bytes = align_up(attend_scratch(*cache, Hq, T, max_len, with_mass != 0)) + kAlign;
+  const long long units = (long long)cache->n_layers * cache->batch * cache->Hkv;
+  const int rows = Hq / cache->Hkv * T;
+  const size_t slots = ta_attend_most_slots(units, rows, max_len);  // of smaller calls too
+  *out_bytes = align_up(ta_attend_sizes_of(units, rows, cache->d, max_len, slots, with_mass != 0).all()) + kAlign;
   return TA_OK;
 }
 

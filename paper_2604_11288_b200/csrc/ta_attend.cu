@@ -50,10 +50,9 @@ struct Shape {
   static constexpr int KS = D / 16;                               // products along d
   static constexpr int RING = W * STAGES * STAGE;
 };
-__host__ __device__ constexpr int rows_of(int MB) { return MB == 0 ? 8 : 16 * MB; }  // query rows of a block
 template <int D, int FMT, int MB, int W>
 constexpr int smem_bytes() {
-  constexpr int R = rows_of(MB);
+  constexpr int R = ta_attend_rows(MB);
   constexpr int q32 = R * D * 4;  // queries in fp32, then (MB > 0) their fragments, hi and lo, in the same place
   constexpr int join = W * R * (D + 4) * 4;
   constexpr int ring = Shape<D, FMT, W>::RING > join ? Shape<D, FMT, W>::RING : join;
@@ -190,8 +189,6 @@ __device__ __forceinline__ int rows_of_unit(const ta_attend_args& a, const Unit&
   return (int)max(0LL, min(asked, most));
 }
 
-constexpr int kJoined = 4096;    // pieces of a row block, times its rows: what the last block joins in shared memory
-constexpr int kPieceUnit = 128;  // cache rows: whole rounds of every variant's four warps
 struct Cut {                     // how the kernel's blocks share the cache rows of a unit's row block
   int pieces, piece, row_blocks;
   int target;               // 0, or: pieces are as long as gives this many in the whole call; `piece` is not used then
@@ -213,7 +210,7 @@ __global__ void __launch_bounds__(W * 32, (MB < 2 ? 12 : 8) / W) ta_attend_kerne
   using S = Shape<D, FMT, W>;
   constexpr int kWarps = W, kThreads = W * 32;
   constexpr bool CODES = S::CODES, NARROW = MB == 0;
-  constexpr int TK = S::TK, NT = TK / 8, KS = S::KS, R = rows_of(MB), MBN = NARROW ? 1 : MB, NR = NARROW ? 1 : 2 * MB;
+  constexpr int TK = S::TK, NT = TK / 8, KS = S::KS, R = ta_attend_rows(MB), MBN = NARROW ? 1 : MB, NR = NARROW ? 1 : 2 * MB;
   constexpr int NJ = D / 8;  // 8-wide tiles of the output
   extern __shared__ __align__(128) uint8_t smem[];
   constexpr int join_bytes = kWarps * R * (D + 4) * 4;
@@ -263,7 +260,7 @@ __global__ void __launch_bounds__(W * 32, (MB < 2 ? 12 : 8) / W) ta_attend_kerne
     __syncthreads();  // (the words are used again)
     all *= cut.groups_per_sequence;
     const int even = (int)((all + cut.target - 1) / cut.target), least = (most + cut.pieces - 1) / cut.pieces;
-    piece = (max(max(even, least), 1) + kPieceUnit - 1) / kPieceUnit * kPieceUnit;
+    piece = (max(max(even, least), 1) + kAttendPieceUnit - 1) / kAttendPieceUnit * kAttendPieceUnit;
   }
   const int n_pieces = max(1, (u.n + piece - 1) / piece);  // at least one, which writes the empty result
   if (part >= n_pieces) return;
@@ -875,7 +872,7 @@ __global__ void __launch_bounds__(W * 32, (MB < 2 ? 12 : 8) / W) ta_attend_kerne
   if (!*s_last) return;
   __threadfence();
   const long long at0 = (long long)group * cut.pieces * R;
-  float2* s_w = reinterpret_cast<float2*>(smem);  // [piece][row], at most kJoined of them: maximum and sum, then what a piece weighs
+  float2* s_w = reinterpret_cast<float2*>(smem);  // [piece][row], at most kAttendJoined of them: maximum and sum, then what a piece weighs
   // Lanes that share a row, all rows at once: a warp per row takes four or eight rows one after another (8 units' 32 query rows
   // over 129 to 4096 rows 23 to 38 us, so 19 to 33, and 18 to 27 with the loads below). With 8 rows a warp has two at most, and the plainer code leaves the loop faster
   // (64 ragged conversations in e4m3 264 us, 281 with the other).
@@ -1007,54 +1004,10 @@ __global__ void __launch_bounds__(256) ta_attend_mass_kernel(ta_attend_args a, S
   }
 }
 
-// How a call is cut: query rows and warps of a block, and pieces of the cache rows. Sized for the 148 SMs of a B200 at two (bf16, or 32
-// query rows) or three blocks each.
-struct Plan {
-  int mb, warps, row_blocks, piece, pieces, target;
-};
-constexpr int kEvenBatch = 1024;  // sequences whose lengths every block adds up
-// The smallest number of pieces that fills whole rounds of resident blocks: a last round with few blocks costs as much as a full
-// one. bf16 is bound by memory and content with 85 % of a round, the 8-bit formats by instructions (95 %). us at 1, 2, 3, 4, 6, 8
-// pieces: 128 units of 32768 bf16 rows 563, 333, 441, 343, 349, 354; 288 units of 16384 e4m3 rows -, 312, 252, 257, 265, -.
-// Where every sequence has a length of its own, and all units fit at once, the pieces are cut on the device from the sum of the
-// lengths, with room for twice as many: 4 x 4 units of 100001 to 131072 int8 rows 154 us, 168 with pieces of max_len / 27 (127 by now); not with
-// more units (512 units of 2048 to 16384 e4m3 rows 308 and 294), whose empty blocks cost more than evenness brings.
-// Many short units: blocks of two warps, twice as many an SM, whose starts and ends weigh half as much (4096 units in a step, us with
-// four and two warps: 17 rows 54 and 40, 65 rows 74 and 59, 257 rows 128 and 122, 4097 rows 1418 and 1403; one warp 36, 53, 121); not where
-// lengths differ much, which longer blocks even out less (4096 units of 100 to 1000 e4m3 rows 165 and 171).
-// With more units than fit at once lengths may differ: four rounds at least (512 units of 2048 to 16384 e4m3 rows
-// -, 331, 312, 293, 294, -; 296 units of 32768 bf16 rows alike lose 1.5 %, 726 to 737).
-Plan plan_of(long long units, int rows, int max_len, bool codes, int ragged_batch) {
-  Plan p;
-  p.mb = rows <= 8 ? 0 : rows <= 16 ? 1 : 2;
-  p.row_blocks = (rows + rows_of(p.mb) - 1) / rows_of(p.mb);
-  const long long groups = units * p.row_blocks, slots = 148 * (p.mb < 2 ? 3 : 2);
-  int most = groups > kAttendTickets || max_len <= kPieceUnit ? 1 : (max_len + kPieceUnit - 1) / kPieceUnit;
-  if (most > kJoined / rows_of(p.mb)) most = kJoined / rows_of(p.mb);
-  int k = 1;
-  for (; k < most; ++k) {
-    const long long blocks = groups * k, rounds = (blocks + slots - 1) / slots;
-    if (groups > slots && rounds < 4 && k < 4) continue;
-    if (blocks * 100 >= rounds * slots * (codes ? 95 : 85)) break;
-    if (rounds > 8) break;
-  }
-  p.piece = ((max_len + k - 1) / k + kPieceUnit - 1) / kPieceUnit * kPieceUnit;
-  if (p.piece < kPieceUnit) p.piece = kPieceUnit;
-  p.pieces = max_len > p.piece ? (max_len + p.piece - 1) / p.piece : 1;
-  p.target = 0;
-  p.warps = p.mb == 0 && p.pieces == 1 && groups >= 4 * slots && (ragged_batch == 0 || max_len <= 512) ? 2 : 4;
-  if (p.pieces > 1 && ragged_batch > 1 && ragged_batch <= kEvenBatch && groups <= slots) {
-    p.target = (int)(groups * p.pieces);
-    p.pieces = 2 * p.pieces < most ? 2 * p.pieces : most;
-  }
-  return p;
-}
-constexpr size_t up(size_t x) { return (x + 255) / 256 * 256; }
-
 template <int D, int FMT, int MB, int W>
-cudaError_t launch(const ta_attend_args& a, const Scratch& sc, const Plan& p, cudaLaunchConfig_t& cfg, ta_dev_status* status) {
+cudaError_t launch(const ta_attend_args& a, const Scratch& sc, const ta_attend_plan& p, cudaLaunchConfig_t& cfg, ta_dev_status* status) {
   constexpr int smem = smem_bytes<D, FMT, MB, W>();
-  static_assert(W < 4 || Shape<D, FMT, W>::RING >= kJoined * 8, "the join's weights take the ring's place");
+  static_assert(W < 4 || Shape<D, FMT, W>::RING >= kAttendJoined * 8, "the join's weights take the ring's place");
   static bool set[64] = {};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -1070,39 +1023,33 @@ cudaError_t launch(const ta_attend_args& a, const Scratch& sc, const Plan& p, cu
                             Cut{p.pieces, p.piece, p.row_blocks, p.target, a.n_layers * a.cache.Hkv * p.row_blocks}, 128u, status);
 }
 template <int D, int FMT>
-cudaError_t launch(const ta_attend_args& a, const Scratch& sc, const Plan& p, cudaLaunchConfig_t& cfg, ta_dev_status* status) {
+cudaError_t launch(const ta_attend_args& a, const Scratch& sc, const ta_attend_plan& p, cudaLaunchConfig_t& cfg, ta_dev_status* status) {
   if (p.mb == 0) return p.warps == 2 ? launch<D, FMT, 0, 2>(a, sc, p, cfg, status) : launch<D, FMT, 0, 4>(a, sc, p, cfg, status);
   if (p.mb == 1) return launch<D, FMT, 1, 4>(a, sc, p, cfg, status);
   return launch<D, FMT, 2, 4>(a, sc, p, cfg, status);
 }
 template <int D>
-cudaError_t launch(const ta_attend_args& a, const Scratch& sc, const Plan& p, cudaLaunchConfig_t& cfg, ta_dev_status* status) {
+cudaError_t launch(const ta_attend_args& a, const Scratch& sc, const ta_attend_plan& p, cudaLaunchConfig_t& cfg, ta_dev_status* status) {
   if (a.cache.format == TA_CACHE_BF16) return launch<D, TA_CACHE_BF16>(a, sc, p, cfg, status);
   if (a.cache.format == TA_CACHE_E4M3) return launch<D, TA_CACHE_E4M3>(a, sc, p, cfg, status);
   return launch<D, TA_CACHE_INT8>(a, sc, p, cfg, status);
 }
 
+// The call's scratch; null: its size alone
 size_t carve(long long units, int rows, int d, int max_len, bool codes, int ragged_batch, bool with_mass, uint8_t* base,
              Scratch* sc) {
-  const Plan p = plan_of(units, rows, max_len, codes, ragged_batch);
-  const size_t slots = p.pieces > 1 ? (size_t)units * p.row_blocks * p.pieces * rows_of(p.mb) : 0;
-  const long long stride = (max_len + 31) / 32 * 32;
-  size_t off = 0;
-  auto take = [&](size_t bytes) {
-    uint8_t* at = base + off;
-    off += up(bytes);
-    return at;
-  };
-  Scratch s = {};
-  s.part = reinterpret_cast<float*>(take(slots * d * 4));
-  s.part_ml = reinterpret_cast<float2*>(take(slots * 8));
-  if (with_mass) {
-    s.score_stride = stride;
-    s.score = reinterpret_cast<float*>(take((size_t)units * rows * stride * 4));
-    s.row_ml = reinterpret_cast<float2*>(take((size_t)units * rows * 8));
+  const ta_attend_plan p = ta_attend_plan_of(units, rows, max_len, codes, ragged_batch);
+  const ta_attend_sizes z = ta_attend_sizes_of(units, rows, d, max_len, ta_attend_slots(p, units), with_mass);
+  if (sc) {
+    sc->part = reinterpret_cast<float*>(base);
+    sc->part_ml = reinterpret_cast<float2*>(base + z.part);
+    if (with_mass) {
+      sc->score_stride = ta_attend_score_stride(max_len);
+      sc->score = reinterpret_cast<float*>(base + z.part + z.part_ml);
+      sc->row_ml = reinterpret_cast<float2*>(base + z.part + z.part_ml + z.score);
+    }
   }
-  if (sc) *sc = s;
-  return off;
+  return z.all();
 }
 
 }  // namespace
@@ -1115,8 +1062,8 @@ cudaError_t ta_launch_attend(const ta_attend_args& a, int* tickets, ta_dev_statu
   const int units = a.n_layers * a.cache.batch * a.cache.Hkv, rows = a.Hq / a.cache.Hkv * a.T;
   const bool codes = a.cache.format != TA_CACHE_BF16;
   const int ragged_batch = a.cache.lens && !a.cache.lens_per_unit ? a.cache.batch : 0;
-  const Plan p = plan_of(units, rows, a.max_len, codes, ragged_batch);
-  Scratch sc;
+  const ta_attend_plan p = ta_attend_plan_of(units, rows, a.max_len, codes, ragged_batch);
+  Scratch sc = {};
   carve(units, rows, a.d, a.max_len, codes, ragged_batch, a.mass != nullptr, a.scratch, &sc);
   sc.ticket = tickets;
   cudaLaunchConfig_t cfg = {};

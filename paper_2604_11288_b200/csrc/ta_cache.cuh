@@ -6,6 +6,7 @@
 #include <cuda_fp8.h>
 #include <stdint.h>
 
+#include "ta_attend_rule.h"
 #include "ta_internal.cuh"
 
 struct ta_cache_dev {  // a ta_cache for kernels: strides of rows in bytes, of scales in floats
@@ -58,7 +59,7 @@ struct ta_attend_args {
   long long mass_stride;
   uint8_t* scratch;
 };
-// ragged_batch: sequences, where every one has a length of its own, else 0
+// What a call takes. ragged_batch: sequences, where every one has a length of its own, else 0
 size_t ta_attend_scratch(int units, int rows, int d, int max_len, bool codes, int ragged_batch, bool with_mass);
 // tickets: kAttendTickets words, zero before and after
 cudaError_t ta_launch_attend(const ta_attend_args& a, int* tickets, ta_dev_status* status, cudaStream_t stream);

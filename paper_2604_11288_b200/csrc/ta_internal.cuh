@@ -45,8 +45,6 @@ struct ta_stream_sync {
   unsigned long long hold_ns;  // 0; in the self-test: how long the first blocks hold their words back
 };
 
-constexpr int kAttendTickets = 16384;  // units and row blocks of an attention call whose cache rows are cut into pieces
-
 struct ta_ctx {
   int device;
   int sm_count;
