@@ -1069,7 +1069,7 @@ cudaError_t ta_launch_attend(const ta_attend_args& a, int* tickets, ta_dev_statu
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   cudaError_t e = a.d == 64 ? launch<64>(a, sc, p, cfg, status) : launch<128>(a, sc, p, cfg, status);
-  if (e != cudaSuccess || !a.mass) return e;
+  if (e != cudaSuccess || !a.mass || a.mass_stride == 0) return e;
   cfg.gridDim = dim3((unsigned)units, (unsigned)((a.mass_stride + 1023) / 1024), 1);
   cfg.blockDim = dim3(256, 1, 1);
   cfg.dynamicSmemBytes = 0;

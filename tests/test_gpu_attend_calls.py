@@ -26,3 +26,19 @@ def test_a_context_for_the_largest_call_is_enough_for_smaller_ones(form):
             assert ta.ta_ctx_poll(h) == ta.TA_OK
             want = run_attend(c, q[:, :B].contiguous(), 1, max_len=most, with_mass=False)  # in a context of its own
             assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("form", ["bf16", "e4m3"])
+@pytest.mark.parametrize("stride", [None, 0, 5])
+def test_a_largest_length_of_zero(form, stride):
+    c, q = Cache(1, 2, 2, 128, 16, 2, form, len_uniform=0), _q(2, 8, 2).to(DEV)
+    s, out = c.struct(), torch.full_like(q, 7.0)
+    lse, mass = torch.full((1, 2, 8, 2), 7.0, device=DEV), torch.full((64,), 7.0, device=DEV)
+    with Ctx(ta.ta_attend_scratch_bytes(s, 8, 2, 0, True)) as h:
+        ta.ta_attend(h, s, 8, 2, 0, 0, True, 0.0, None, ta.view(q), ta.view(out), lse, None if stride is None else mass, stride or 0,
+                     torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        assert ta.ta_ctx_poll(h) == ta.TA_OK
+    assert (out == 0).all() and (lse == -torch.inf).all()
+    written = 4 * (stride or 0)  # of every sequence and head
+    assert (mass[:written] == 0).all() and (mass[written:] == 7.0).all()
