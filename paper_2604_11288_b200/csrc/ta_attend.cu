@@ -968,7 +968,7 @@ __global__ void __launch_bounds__(W * 32, (MB < 2 ? 12 : 8) / W) ta_attend_kerne
 }
 
 // Attention mass per cache row, from the scores and the rows' maxima and sums; a thread has four cache rows. grid.x = units,
-// grid.y = stretches of 1024 rows. (Formed at the end of the attention's own blocks, where a unit is one block, it took longer:
+// grid.y = stretches of 1024 rows, or as many as a grid can have. (Formed at the end of the attention's own blocks, where a unit is one block, it took longer:
 // 32 x 16 x 8 units of 257 rows 135 us a step where this takes 128, of 1025 rows 423 and 388.)
 __global__ void __launch_bounds__(256) ta_attend_mass_kernel(ta_attend_args a, Scratch sc) {
   ta_wait_for_prior_grid();
@@ -1070,7 +1070,8 @@ cudaError_t ta_launch_attend(const ta_attend_args& a, int* tickets, ta_dev_statu
   cfg.numAttrs = 1;
   cudaError_t e = a.d == 64 ? launch<64>(a, sc, p, cfg, status) : launch<128>(a, sc, p, cfg, status);
   if (e != cudaSuccess || !a.mass || a.mass_stride == 0) return e;
-  cfg.gridDim = dim3((unsigned)units, (unsigned)((a.mass_stride + 1023) / 1024), 1);
+  const long long stretches = (a.mass_stride + 1023) / 1024;
+  cfg.gridDim = dim3((unsigned)units, (unsigned)(stretches < 65535 ? stretches : 65535), 1);
   cfg.blockDim = dim3(256, 1, 1);
   cfg.dynamicSmemBytes = 0;
   return cudaLaunchKernelEx(&cfg, ta_attend_mass_kernel, a, sc);

@@ -42,3 +42,18 @@ def test_a_largest_length_of_zero(form, stride):
     assert (out == 0).all() and (lse == -torch.inf).all()
     written = 4 * (stride or 0)  # of every sequence and head
     assert (mass[:written] == 0).all() and (mass[written:] == 7.0).all()
+
+
+def test_more_room_for_the_mass_than_a_grid_is_high():
+    stride = 65535 * 1024 + 4
+    c, q = Cache(1, 1, 1, 128, 16, 2, lens=[21]), _q(1, 2, 1).to(DEV)
+    want = run_attend(c, q, 1)[2]
+    mass, out = torch.full((stride + 8,), 7.0, device=DEV), torch.empty_like(q)
+    s = c.struct()
+    with Ctx(ta.ta_attend_scratch_bytes(s, 2, 1, 32, True)) as h:
+        ta.ta_attend(h, s, 2, 1, 0, 32, True, 0.0, None, ta.view(q), ta.view(out), None, mass, stride,
+                     torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        assert ta.ta_ctx_poll(h) == ta.TA_OK
+    assert torch.equal(mass[:32].cpu().double(), want[0, 0, 0]) and int(mass[32:stride].count_nonzero()) == 0
+    assert (mass[stride:] == 7.0).all()
