@@ -571,7 +571,7 @@ ta_status ta_cache_read(ta_ctx* ctx, const ta_cache* cache, const ta_batch* batc
  * A query that sees no row gets out 0, lse -infinity and adds no mass. What rows beyond a query's last one hold, NaN
  * included, has no influence on it. A sequence with n > max_len or beyond its table is cut there, and rows in a page
  * outside 0..n_pages-1 are left out; both are reported (TA_ERR_DEVICE_BOUNDS). T <= TA_MAX_NEW_TOKENS, Hq / Hkv <= 256,
- * max_len <= TA_MAX_SEQ_LEN. Products are of bf16 values (8-bit codes are exact in them; probabilities and rotated queries
+ * max_len <= TA_MAX_SEQ_LEN, (layer, sequence, KV head) times blocks of 32 query rows below 2^31. Products are of bf16 values (8-bit codes are exact in them; probabilities and rotated queries
  * keep 16 bits), sums and softmax statistics are in 32 bits; the same call on the same inputs gives the same bits. Scratch:
  * ta_attend_scratch_bytes, enough for every call that is no larger in layers, sequences, KV heads, query heads of a KV head, T and
  * max_len, with mass or, where with_mass is 0, without; at most 92 MB beside what the mass takes (4 bytes for every query head, token

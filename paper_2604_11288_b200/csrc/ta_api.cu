@@ -1174,6 +1174,9 @@ ta_status check_attend(const ta_cache* c, int Hq, int T, int max_len) {
   if (s != TA_OK) return s;
   if (Hq < c->Hkv || Hq % c->Hkv || T < 1 || max_len < 0) return TA_ERR_INVALID_ARG;
   if (T > TA_MAX_NEW_TOKENS || Hq / c->Hkv > 256 || max_len > TA_MAX_SEQ_LEN) return TA_ERR_UNSUPPORTED;
+  // a block for every unit and block of query rows at least
+  const int rows = Hq / c->Hkv * T, block = ta_attend_rows(ta_attend_mb(rows));
+  if ((long long)c->n_layers * c->batch * c->Hkv * ((rows + block - 1) / block) > 0x7fffffffLL) return TA_ERR_UNSUPPORTED;
   return TA_OK;
 }
 }  // namespace

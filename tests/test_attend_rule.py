@@ -106,3 +106,12 @@ def test_plans_cover_their_rows(rule):
         assert pieces == 1 or units * row_blocks <= 16384  # a counter each
         assert warps == 4 or (warps == 2 and mb == 0 and pieces == 1)
         assert target == 0 or (pieces > 1 and 1 < ragged <= 1024)
+
+
+def test_more_blocks_than_a_grid_has_are_refused(lib):
+    ok = _cache(1 << 20, layers=16)  # 2^27 units
+    assert ta.ta_attend_scratch_bytes(ok, 8 * 256, 1, 100) > 0
+    for T in (2, 64):
+        with pytest.raises(ta.TAError) as e:
+            ta.ta_attend_scratch_bytes(ok, 8 * 256, T, 100)
+        assert e.value.status == ta.TA_ERR_UNSUPPORTED
