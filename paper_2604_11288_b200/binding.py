@@ -491,15 +491,20 @@ _FORMATS = {"torch.bfloat16": TA_CACHE_BF16, "torch.float8_e4m3fn": TA_CACHE_E4M
 
 def make_cache(k, v, k_scale=None, v_scale=None, table=None, batch=None, lens=None, len_uniform=0) -> ta_cache:
     """ta_cache over tensors k and v [L, pages, Hkv, page, d] (bfloat16, float8_e4m3fn or int8, any strides with d contiguous,
-    the same for both) with scales [L, pages, Hkv, page] for the 8-bit types. table [B, pages_per_seq] int32, or None: every
+    the same for both) with float32 scales [L, pages, Hkv, page] for the 8-bit types. table [B, pages_per_seq] int32, or None: every
     sequence owns pages / batch pages in a row. lens [B] or [L, B, Hkv] int32, or None: len_uniform. The tensors must outlive it."""
     assert str(k.dtype) in _FORMATS and k.dtype == v.dtype, "keys and values are bfloat16, float8_e4m3fn or int8 alike"
     assert k.dim() == 5 and k.shape == v.shape and k.stride() == v.stride() and k.stride(4) == 1, "k and v must be laid out alike"
     L, pages, Hkv, page, d = k.shape
     scales = (0, 0, 0, 0)
-    if k_scale is not None:
-        assert tuple(k_scale.shape) == (L, pages, Hkv, page) == tuple(v_scale.shape) and k_scale.stride() == v_scale.stride()
+    with_scales = k.dtype.itemsize == 1
+    assert with_scales == (k_scale is not None) == (v_scale is not None), "the 8-bit types have scales of both, bfloat16 has none"
+    if with_scales:
+        assert str(k_scale.dtype) == "torch.float32" == str(v_scale.dtype), "scales are float32"
+        assert tuple(k_scale.shape) == (L, pages, Hkv, page) == tuple(v_scale.shape) and k_scale.stride() == v_scale.stride(), \
+            "a scale for every row, those of keys and values laid out alike"
         scales = k_scale.stride()
+    assert all(t is None or str(t.dtype) == "torch.int32" for t in (table, lens)), "page numbers and lengths are int32"
     if table is not None:
         assert table.dim() == 2 and table.stride(1) == 1 and (table.shape[0] == 1 or table.stride(0) == table.shape[1])
         batch, wide = table.shape
