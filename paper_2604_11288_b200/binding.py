@@ -257,6 +257,11 @@ def _ptr(t):
     return t.ctypes.data
 
 
+def _is(t, *dtypes):
+    """Whether a tensor or array, if there is one, has one of these types. (Of a bare address nothing is known.)"""
+    return t is None or isinstance(t, int) or str(t.dtype).removeprefix("torch.") in dtypes
+
+
 def view(t, ragged=False) -> ta_bf16_view:
     """ta_bf16_view of a bf16 tensor [L, B, H, n, d] (uniform) or [L, H, total, d] (ragged); strides in elements."""
     return (_call or _native()).view(t, ragged)
@@ -470,6 +475,10 @@ def ta_ctx_selftest_step_wait(ctx, pats, policy, st: ta_stream, new_ids, attn, e
 
 def ta_rotary_table(d_rot, base, scaling, factor, original_len, low, high, phase) -> float:
     """Fills phase (host, d_rot // 2 64-bit integers: a numpy array or a CPU tensor) and returns the factor on rotated values."""
+    assert _is(phase, "int64", "uint64"), "frequencies are 64-bit integers"
+    if hasattr(phase, "dtype"):
+        in_a_row = phase.is_contiguous() if hasattr(phase, "is_contiguous") else phase.flags.c_contiguous
+        assert in_a_row and len(phase) >= d_rot // 2, "d_rot // 2 64-bit integers in a row are written"
     out = C.c_float(0.0)
     _check(lib().ta_rotary_table(d_rot, base, scaling, factor, original_len, low, high, _ptr(phase), C.byref(out)),
            "ta_rotary_table")
@@ -477,7 +486,9 @@ def ta_rotary_table(d_rot, base, scaling, factor, original_len, low, high, phase
 
 
 def make_rotary(phase, d_rot, layout=TA_ROTARY_HALF, magnitude=1.0, inverse=False, positions=None) -> ta_rotary:
-    """ta_rotary over a device copy of ta_rotary_table's phases. The tensors must outlive it."""
+    """ta_rotary over a device copy of ta_rotary_table's phases, with int32 positions. The tensors must outlive it."""
+    assert _is(phase, "int64", "uint64"), "frequencies are 64-bit integers"
+    assert _is(positions, "int32"), "positions are int32"
     return ta_rotary(_ptr(phase), _ptr(positions), d_rot, layout, 1 if inverse else 0, magnitude)
 
 
@@ -500,11 +511,11 @@ def make_cache(k, v, k_scale=None, v_scale=None, table=None, batch=None, lens=No
     with_scales = k.dtype.itemsize == 1
     assert with_scales == (k_scale is not None) == (v_scale is not None), "the 8-bit types have scales of both, bfloat16 has none"
     if with_scales:
-        assert str(k_scale.dtype) == "torch.float32" == str(v_scale.dtype), "scales are float32"
+        assert _is(k_scale, "float32") and _is(v_scale, "float32"), "scales are float32"
         assert tuple(k_scale.shape) == (L, pages, Hkv, page) == tuple(v_scale.shape) and k_scale.stride() == v_scale.stride(), \
             "a scale for every row, those of keys and values laid out alike"
         scales = k_scale.stride()
-    assert all(t is None or str(t.dtype) == "torch.int32" for t in (table, lens)), "page numbers and lengths are int32"
+    assert _is(table, "int32") and _is(lens, "int32"), "page numbers and lengths are int32"
     if table is not None:
         assert table.dim() == 2 and table.stride(1) == 1 and (table.shape[0] == 1 or table.stride(0) == table.shape[1])
         batch, wide = table.shape

@@ -1,4 +1,5 @@
 """Types that the descriptions of caches and rotations insist on: what is described reaches the kernels as an address."""
+import numpy as np
 import pytest
 import torch
 
@@ -31,3 +32,17 @@ def test_scales_are_float32_and_go_with_8_bits(dtype):
     for a, b in ((s, s), (s, None), (None, s)):
         with pytest.raises(AssertionError, match="scale"):
             ta.make_cache(k, k, a, b, batch=2)
+
+
+def test_frequencies_and_positions():
+    for phase in (torch.zeros(64, dtype=torch.int64), torch.zeros(64, dtype=torch.uint64), np.zeros(64, dtype=np.uint64)):
+        assert ta.ta_rotary_table(128, 10000.0, ta.TA_SCALING_PLAIN, 1.0, 0.0, 0.0, 0.0, phase) == 1.0
+        assert ta.make_rotary(phase, 128, positions=torch.zeros(3, dtype=torch.int32)).d_rot == 128
+    for phase in (torch.zeros(63, dtype=torch.int64), torch.zeros(64, dtype=torch.float32), torch.zeros(64, dtype=torch.float64),
+                  torch.zeros(128, dtype=torch.int64)[::2], np.zeros(64, dtype=np.uint32), np.zeros(63, dtype=np.uint64)):
+        with pytest.raises(AssertionError, match="64-bit"):
+            ta.ta_rotary_table(128, 10000.0, ta.TA_SCALING_PLAIN, 1.0, 0.0, 0.0, 0.0, phase)
+    with pytest.raises(AssertionError, match="64-bit"):
+        ta.make_rotary(torch.zeros(64), 128)
+    with pytest.raises(AssertionError, match="int32"):
+        ta.make_rotary(torch.zeros(64, dtype=torch.int64), 128, positions=torch.zeros(3, dtype=torch.int64))
