@@ -120,7 +120,7 @@ __global__ void __launch_bounds__(kThreads, 8) ta_cache_append_kernel(ta_cache_m
   // positions looked up once a token, behind the places (2662 us, beside them 2870), or, in a call with few rows, once an angle,
   // beside them (64 tokens 7.1 us, 7.4 behind)
   constexpr bool ONCE = ITEMS == kItems;
-  extern __shared__ float2 s_cs[];  // [token][pair]
+  extern __shared__ __align__(16) float2 s_cs[];  // [token][pair]
   __shared__ Place s_place[ITEMS];
   __shared__ int s_position[ITEMS];
   __shared__ Kept s_kept;

@@ -49,7 +49,7 @@ template <int V, bool INTER>
 __global__ void __launch_bounds__(kThreads) ta_rotate_kernel(ta_rotate_args a, Cut cut) {
   ta_wait_for_prior_grid();
   ta_launch_dependents();
-  extern __shared__ float2 s_cs[];  // [token][pair]
+  extern __shared__ __align__(16) float2 s_cs[];  // [token][pair]
   const int l = blockIdx.y, half = a.rot.d_rot / 2;
   const long long tok0 = (long long)blockIdx.x * cut.tokens;
   const int tokens = (int)min((long long)cut.tokens, a.seq.total - tok0);
