@@ -16,4 +16,4 @@ def test_dynamic_shared_memory_is_declared_aligned():
             found += 1
             rounded_up = re.search(rf"\(uintptr_t\){name} \+ \d+\) & ~", src)
             assert (align and int(align) >= 16) or rounded_up, (os.path.basename(path), name)
-    assert found == 6
+    assert found >= 7
