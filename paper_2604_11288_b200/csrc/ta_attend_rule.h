@@ -21,7 +21,6 @@ constexpr long long ta_attend_resident(int mb) { return 148 * (mb < 2 ? 3 : 2); 
 struct ta_attend_plan {
   int mb, warps, row_blocks, piece, pieces, target;
 };
-constexpr int kAttendEvenBatch = 1024;  // sequences whose lengths every block adds up
 // The smallest number of pieces that fills whole rounds of resident blocks: a last round with few blocks costs as much as a full
 // one. bf16 is bound by memory and content with 85 % of a round, the 8-bit formats by instructions (95 %). us at 1, 2, 3, 4, 6, 8
 // pieces: 128 units of 32768 bf16 rows 563, 333, 441, 343, 349, 354; 288 units of 16384 e4m3 rows -, 312, 252, 257, 265, -.
@@ -52,7 +51,7 @@ inline ta_attend_plan ta_attend_plan_of(long long units, int rows, int max_len, 
   p.pieces = max_len > p.piece ? (max_len + p.piece - 1) / p.piece : 1;
   p.target = 0;
   p.warps = p.mb == 0 && p.pieces == 1 && groups >= 4 * slots && (ragged_batch == 0 || max_len <= 512) ? 2 : 4;
-  if (p.pieces > 1 && ragged_batch > 1 && ragged_batch <= kAttendEvenBatch && groups <= slots) {
+  if (p.pieces > 1 && ragged_batch > 1 && groups <= slots) {  // (every block adds up the lengths of as many sequences)
     p.target = (int)(groups * p.pieces);
     p.pieces = 2 * p.pieces < most ? 2 * p.pieces : most;
   }
