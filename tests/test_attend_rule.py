@@ -115,3 +115,21 @@ def test_more_blocks_than_a_grid_has_are_refused(lib):
         with pytest.raises(ta.TAError) as e:
             ta.ta_attend_scratch_bytes(ok, 8 * 256, T, 100)
         assert e.value.status == ta.TA_ERR_UNSUPPORTED
+
+
+def test_the_variants_that_calls_of_these_sizes_take(rule):
+    """What the tests of the variants rely on: [query rows of a block / 16, warps, row blocks, piece, pieces, cut on the device]."""
+    out = (ctypes.c_int * 6)()
+
+    def plan(*args):
+        rule.plan(*args, out)
+        return list(out)[:2] + [out[4], out[5] > 0]
+    for codes, ragged in itertools.product((0, 1), (0, 75)):
+        assert plan(1800, 8, 70, codes, ragged) == [0, 2, 1, False]      # many short units
+        assert plan(1920, 4, 65, codes, ragged) == [0, 2, 1, False]
+        assert plan(2560, 4, 257, codes, 0) == [0, 2, 1, False]
+        assert plan(16408, 8, 150, codes, 2051) == [0, 2, 1, False]      # more row blocks than counters
+        assert plan(16408, 16, 150, codes, 2051)[2:] == plan(8240, 64, 150, codes, 1030)[2:] == [1, False]
+        for rows in (4, 16, 32):
+            assert plan(512, rows, 1100, codes, 64)[2] > 1 and not out[5]  # more units than run at once, in pieces
+        assert [plan(b, 4, 400, codes, b)[3] for b in (1, 2, 222, 377, 444, 445)] == [False, True, True, True, False, False]
