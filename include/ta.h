@@ -567,17 +567,20 @@ ta_status ta_cache_read(ta_ctx* ctx, const ta_cache* cache, const ta_batch* batc
  *   lse     DEVICE float [L][B][Hq][T], natural log, out; or NULL
  *   mass    DEVICE float [L][B][Hkv][mass_stride], out, or NULL: sum of p_j over the unit's query heads and tokens, zero for
  *           rows n..mass_stride-1 (mass_stride >= max_len): ta_stream_step's `attn` with mass_stride = K+1
- *   max_len >= every n
+ *   max_len >= every n. The work is shared out by it: a bound far above the lengths costs time
  * A query that sees no row gets out 0, lse -infinity and adds no mass. What rows beyond a query's last one hold, NaN
- * included, has no influence on it. A sequence with n > max_len or beyond its table is cut there, and rows in a page
+ * included, has no influence on it. A NaN that it sees is told; an infinity that it sees (bf16) may come out as NaN too, since
+ * factors enter products in two parts. A sequence with n > max_len or beyond its table is cut there, and rows in a page
  * outside 0..n_pages-1 are left out; both are reported (TA_ERR_DEVICE_BOUNDS). T <= TA_MAX_NEW_TOKENS, Hq / Hkv <= 256,
- * max_len <= TA_MAX_SEQ_LEN, (layer, sequence, KV head) times blocks of 32 query rows below 2^31. Products are of bf16 values (8-bit codes are exact in them; probabilities and rotated queries
- * keep 16 bits), sums and softmax statistics are in 32 bits; the same call on the same inputs gives the same bits. Scratch:
- * ta_attend_scratch_bytes, enough for every call that is no larger in layers, sequences, KV heads, query heads of a KV head, T and
- * max_len, with mass or, where with_mass is 0, without; at most 92 MB beside what the mass takes (4 bytes for every query head, token
- * and cache row). It is not kept between calls; what ta_compress keeps under a seq_epoch is dropped. Calls of one context share it
- * and the counters by which blocks join: order calls on different streams. The two codes of E4M3 that mean NaN, which
- * ta_cache_append does not write, count as 480 here. */
+ * max_len <= TA_MAX_SEQ_LEN, (layer, sequence, KV head) times blocks of 32 query rows below 2^31.
+ * Products are of 16-bit values: 8-bit codes are exact in them, probabilities and rotated queries keep 16 bits, and queries over
+ * an 8-bit cache are taken to 2^-24 of the largest value of their head. Sums and softmax statistics are in 32 bits; the same call
+ * on the same inputs gives the same bits.
+ * Scratch: ta_attend_scratch_bytes, enough for every call that is no larger in layers, sequences, KV heads, query heads of a KV
+ * head, T and max_len, with mass or, where with_mass is 0, without; at most 92 MB beside what the mass takes (4 bytes for every
+ * query head, token and cache row). It is not kept between calls; what ta_compress keeps under a seq_epoch is dropped. Calls of one
+ * context share it and the counters by which blocks join: order calls on different streams. The two codes of E4M3 that mean NaN,
+ * which ta_cache_append does not write, count as 480 here. */
 enum { TA_MAX_NEW_TOKENS = 64 };
 ta_status ta_attend_scratch_bytes(const ta_cache* cache, int Hq, int T, int max_len, int with_mass, size_t* out_bytes);
 ta_status ta_attend(ta_ctx* ctx, const ta_cache* cache, int Hq, int T, int new_rows, int max_len, int causal, float scale,

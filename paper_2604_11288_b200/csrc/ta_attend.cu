@@ -20,8 +20,9 @@
 // which would be empty, holds the lo parts at no cost (MB = 0); with more rows the lo parts are a second product.
 //
 // What bounds it. bf16: memory, 16 x 32768 rows of 8 heads in 306 us, 7.0 TB/s. 8-bit: instructions, 940 for a tile of 32 rows, of
-// which 384 turn codes into fp16 and 64 are products: 36 x 16384 e4m3 rows of 8 heads 225 us, 5.5 TB/s; with 16 query rows 1200 or so
-// (8 x 131072 int8 rows of 4 heads 289 us, 3.8 TB/s). Cache rows as the long side of the products (S^T = K Q^T, half of them and of the
+// which 384 turn codes into fp16 and 64 are products: 36 x 16384 e4m3 rows of 8 heads 225 us, 5.5 TB/s. With 16 query rows 1170 for a
+// tile, and latency: issue slots 52 % taken, tensor cores 46 %, memory 41 %, three warps a scheduler that wait for their own
+// results (4 x 100001 to 131072 int8 rows of 4 heads 130 us, 3.6 TB/s). Cache rows as the long side of the products (S^T = K Q^T, half of them and of the
 // accumulators, four blocks an SM instead of three) were slower, 275 us where this took 238: no fewer instructions, and less
 // distance between those that depend on one another. Tiles of 16 rows for codes: 297 for 251. Bulk copies for codes: 511 for 296 row by
 // row, 247 for 250 in runs of 16 rows.
@@ -132,7 +133,8 @@ __device__ __forceinline__ uint32_t rest2(float x, float y, uint32_t hi) {
 //     mantissa bits stand where fp16 has the last four and first three of its own, the sign that lands on the fifth exponent
 //     bit masked out: the value times 2^-8 (kCodeUnit), subnormals included. The shift is a product with a number that the
 //     compiler does not know: the other two instructions load the integer pipe, this one the multipliers.
-//   INT8: the byte with its upper bit turned over is c + 128; under the exponent of 1024 that is 1152 + c, less 1152.
+//   INT8: the byte with its upper bit turned over is c + 128; under the exponent of 1024 that is 1152 + c, less 1152. (A number put under
+//     the exponent that makes its unit the mantissa's last place: a published way to convert integers, the constants follow from fp16.)
 template <int FMT, int I>
 __device__ __forceinline__ uint32_t pair_of(uint32_t x, uint32_t y, uint32_t times128) {
   if constexpr (FMT == TA_CACHE_E4M3) {

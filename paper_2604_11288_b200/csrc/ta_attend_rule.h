@@ -16,8 +16,8 @@ TA_ATTEND_RULE constexpr int ta_attend_rows(int mb) { return mb == 0 ? 8 : 16 * 
 constexpr int ta_attend_mb(int rows) { return rows <= 8 ? 0 : rows <= 16 ? 1 : 2; }              // for so many of a unit
 constexpr long long ta_attend_resident(int mb) { return 148 * (mb < 2 ? 3 : 2); }                // blocks on the device at once
 
-// How a call is cut: query rows and warps of a block, and pieces of the cache rows. Sized for the 148 SMs of a B200 at two (bf16, or 32
-// query rows) or three blocks each.
+// How a call is cut: query rows and warps of a block, and pieces of the cache rows. Sized for the 148 SMs of a B200 at three blocks
+// each, two with 32 query rows.
 struct ta_attend_plan {
   int mb, warps, row_blocks, piece, pieces, target;
 };
@@ -28,8 +28,10 @@ struct ta_attend_plan {
 // lengths, with room for twice as many: 4 x 4 units of 100001 to 131072 int8 rows 154 us, 168 with pieces of max_len / 27 (127 by now); not with
 // more units (512 units of 2048 to 16384 e4m3 rows 308 and 294), whose empty blocks cost more than evenness brings.
 // Many short units: blocks of two warps, twice as many an SM, whose starts and ends weigh half as much (4096 units in a step, us with
-// four and two warps: 17 rows 54 and 40, 65 rows 74 and 59, 257 rows 128 and 122, 4097 rows 1418 and 1403; one warp 36, 53, 121); not where
-// lengths differ much, which longer blocks even out less (4096 units of 100 to 1000 e4m3 rows 165 and 171).
+// four and two warps: 17 rows 54 and 40, 65 rows 74 and 59, 257 rows 128 and 122, 4097 rows 1418 and 1403; one warp 36, 53, 121); only up to
+// 512 rows where lengths differ, which longer blocks even out less (4096 units, longest eight times the shortest, four and two warps: 256
+// rows e4m3 90 and 85, bf16 86 and 75; 512 rows 117.0 and 116.0, 118 and 112; 768 rows 142.1 and 142.5, 155.8 and 156.2; 1024 rows 172 and
+// 177, 208 and 213).
 // With more units than fit at once lengths may differ: four rounds at least (512 units of 2048 to 16384 e4m3 rows
 // -, 331, 312, 293, 294, -; 296 units of 32768 bf16 rows alike lose 1.5 %, 726 to 737).
 inline ta_attend_plan ta_attend_plan_of(long long units, int rows, int max_len, bool codes, int ragged_batch) {
