@@ -19,7 +19,7 @@
 // enter their products as a sum of two 16-bit parts, hi + lo: with up to 8 query rows the lower half of the 16-row product,
 // which would be empty, holds the lo parts at no cost (MB = 0); with more rows the lo parts are a second product.
 //
-// What bounds it. bf16: memory, 16 x 32768 rows of 8 heads in 306 us, 7.0 TB/s. 8-bit: instructions, 940 for a tile of 32 rows, of
+// What bounds it. bf16: memory, 16 x 32768 rows of 8 heads in 306 us, 7.0 TB/s. 8-bit: instructions, 914 for a tile of 32 rows, of
 // which 384 turn codes into fp16 and 64 are products: 36 x 16384 e4m3 rows of 8 heads 225 us, 5.5 TB/s. With 16 query rows 1170 for a
 // tile, and latency: issue slots 52 % taken, tensor cores 46 %, memory 41 %, three warps a scheduler that wait for their own
 // results (4 x 100001 to 131072 int8 rows of 4 heads 130 us, 3.6 TB/s). Cache rows as the long side of the products (S^T = K Q^T, half of them and of the
